@@ -280,6 +280,116 @@ psc_status psc_conv3x3_bwd_weight(const psc_layer *layer, const psc_packed *pack
                                   int32_t n, int32_t h, int32_t w, float *d_dvalues,
                                   float *d_dbias, void *d_ws, size_t ws_bytes, void *stream);
 
+/* ---- Group normalisation with an activation, between the convolutions of a
+ * network that is trained or retrained.  Activations are [n][c][h][w]
+ * (PSC_NCHW, what the convolutions read and write) or [n][h][w][c]
+ * (PSC_NHWC), fp32 or fp16; gamma, beta, the statistics and the parameters'
+ * gradients are fp32 for both, and all sums are.  Image n, group g of
+ * c / groups neighbouring channels, over its M = c / groups * h * w values:
+ *   mean = sum x / M,  rstd = 1 / sqrt(sum (x - mean)^2 / M + eps),
+ *   xhat = (x - mean) rstd,  u = gamma[c] xhat + beta[c],  y = act(u)
+ * with act(u) = u, max(u, 0) or u / (1 + exp(-u)). */
+typedef enum { PSC_NCHW = 0, PSC_NHWC = 1 } psc_layout;
+typedef enum { PSC_ACT_NONE = 0, PSC_ACT_RELU = 1, PSC_ACT_SILU = 2 } psc_act;
+
+/* Bytes of workspace of the forward (backward == 0) or backward call of these
+ * sizes (0 is a valid answer); 256-byte aligned, it holds nothing from one
+ * call to the next, and calls that may overlap need one each. */
+psc_status psc_group_norm_workspace(int32_t dtype, int32_t layout, int32_t n, int32_t c, int32_t h,
+                                    int32_t w, int32_t groups, int32_t backward, size_t *bytes);
+
+/* d_y = act(u).  d_gamma and d_beta [c] may be NULL (1 and 0).  d_mean and
+ * d_rstd [n][groups] receive the statistics that the backward reads; both may
+ * be NULL.  groups divides c; eps is positive and finite.  d_y must not
+ * overlap d_x.  n == 0 is a no-op.  A group with a value that is not finite
+ * has NaN statistics and outputs; other groups are not touched by it. */
+psc_status psc_group_norm_fwd(int32_t dtype, int32_t layout, const void *d_x, int32_t n, int32_t c,
+                              int32_t h, int32_t w, int32_t groups, const float *d_gamma,
+                              const float *d_beta, float eps, int32_t act, void *d_y, float *d_mean,
+                              float *d_rstd, void *d_ws, size_t ws_bytes, void *stream);
+
+/* The backward of that call from the gradient d_dy of its output (layout and
+ * dtype of d_x) and its statistics: with du = dy act'(u) (act'(0) = 0 for the
+ * ReLU),
+ *   d_dgamma[c] = sum du xhat,  d_dbeta[c] = sum du   (over n, h, w),
+ *   d_dx = rstd (gamma du - (sum gamma du + xhat sum gamma du xhat) / M),
+ * the inner sums over the group.  d_dgamma and d_dbeta are written in full, in
+ * a fixed order of sums (reproducible bit for bit); each may be NULL.  d_dx
+ * must not overlap d_x or d_dy.  n == 0 writes zeros to d_dgamma and d_dbeta. */
+psc_status psc_group_norm_bwd(int32_t dtype, int32_t layout, const void *d_x, const void *d_dy,
+                              int32_t n, int32_t c, int32_t h, int32_t w, int32_t groups,
+                              const float *d_gamma, const float *d_beta, const float *d_mean,
+                              const float *d_rstd, int32_t act, void *d_dx, float *d_dgamma,
+                              float *d_dbeta, void *d_ws, size_t ws_bytes, void *stream);
+
+/* ---- The optimiser of the retraining: AdamW over many tensors in one call
+ * (the stored values of packed layers, whose gradient is
+ * psc_conv3x3_bwd_weight's, biases, norm parameters, dense weights), and the
+ * norm of all their gradients.  The list is host memory, read before the call
+ * returns; the addresses in it go to the kernels as arguments, so a captured
+ * call replays on the same tensors.  Tensors need only the alignment of their
+ * elements; 16 bytes (8 for fp16, 4 for 8-bit codes) is fastest.  No tensor
+ * of a list may overlap another that the call writes. */
+typedef struct psc_param {
+    float *param;         /* [numel], updated in place */
+    const void *grad;     /* [numel], grad_dtype */
+    void *copy;           /* [numel] fp16: receives the new parameter, rounded (the
+                             values of an fp16 layer, say); may be NULL */
+    void *m, *v;          /* [numel] the moments, updated in place, all zero before
+                             the first step: fp32, or with state_bits 8 int8 and
+                             uint8 codes */
+    float *scale;         /* state_bits 8: [ceil(numel/256)][2], 8-byte aligned, all
+                             zero before the first step; else not read */
+    int64_t numel;        /* 0..2^31-1 */
+    float weight_decay;   /* of this tensor, finite, >= 0 */
+    int32_t grad_dtype;   /* psc_dtype */
+    int32_t state_bits;   /* 32 or 8 */
+    int32_t reserved;     /* 0 */
+} psc_param;
+
+typedef struct psc_adamw {
+    float lr, beta1, beta2, eps;  /* finite; 0 <= beta < 1; eps >= FLT_MIN */
+    const float *d_lr;            /* device: read in the place of lr; NULL: lr */
+} psc_adamw;
+
+/* d_out[0] = norm = scale * sqrt(sum over all tensors of g^2), the squares
+ * summed in fp64 in a fixed order, and d_out[1] = scale * min(1, max_norm /
+ * norm): the factor that unscales gradients 1 / scale times too large and
+ * clips them to max_norm.  Where the norm is not finite the factor is NaN.
+ * scale is positive and finite, max_norm positive, or infinite to clip
+ * nothing.  Of each entry only grad, numel and grad_dtype are read.  d_ws:
+ * PSC_GRAD_NORM_WS_BYTES bytes, 256-byte aligned; calls that may overlap need
+ * one each. */
+#define PSC_GRAD_NORM_WS_BYTES 8192
+psc_status psc_grad_norm(const psc_param *h_params, int32_t count, float scale, float max_norm,
+                         float *d_out, void *d_ws, size_t ws_bytes, void *stream);
+
+/* One step, t = the steps done plus this one, for every tensor:
+ *   g = *d_factor * grad                (d_factor NULL: 1)
+ *   m = beta1 m + (1 - beta1) g,  v = beta2 v + (1 - beta2) g^2
+ *   param = param - lr weight_decay param
+ *           - lr / (1 - beta1^t) * m / (sqrt(v / (1 - beta2^t)) + eps)
+ * If *d_factor is not finite nothing is changed and no step is counted.
+ * d_state: PSC_ADAMW_STATE_BYTES bytes of the optimiser's, 256-byte aligned,
+ * all zero before the first step; its first 8 bytes are the steps done
+ * (int64).  Calls with one state must not overlap.
+ *
+ * With state_bits 8 the moments of 256 elements in a row share two scales,
+ * their largest |m| and largest v: m's code q in -127..127 stands for
+ * sign(q) (q / 127)^2 scale[0], v's code in 0..255 for (c / 255)^4 scale[1].
+ * The step computes with what they stand for in fp64, updates the parameter
+ * with the new moments before they are rounded, and rounds sqrt|m| and
+ * v^(1/4) to the nearest code; v > 0 keeps a code above 0.  A gradient that is
+ * not finite spoils the moments of its 256 elements (with 32 bits: its own). */
+#define PSC_ADAMW_STATE_BYTES 64
+psc_status psc_adamw_step(const psc_param *h_params, int32_t count, const psc_adamw *opt,
+                          const float *d_factor, void *d_state, void *stream);
+
+/* The values that 8-bit moments stand for: numel codes and their scales, as in
+ * psc_param, to fp32 d_m_out and d_v_out [numel]. */
+psc_status psc_adamw_moments(const void *d_m, const void *d_v, const float *d_scale, int64_t numel,
+                             float *d_m_out, float *d_v_out, void *stream);
+
 /* ---- Data-free ADMM pattern pruning of one layer (Sec. 4.3, Eq. 4-7;
  * Algorithm 1).  With input X (synthetic data), pre-trained W0, b0 and
  * target X' = relu(W0 X + b0) (psc_dense3x3_fwd with relu), an iteration is

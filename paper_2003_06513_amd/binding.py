@@ -23,6 +23,8 @@ PSC_OK, PSC_ERR_ARG, PSC_ERR_UNSUPPORTED, PSC_ERR_WORKSPACE, PSC_ERR_DEVICE, PSC
 PSC_F32, PSC_F16 = 0, 1
 PSC_OP_SELECT, PSC_OP_PACK = 0, 1
 MAX_PATTERNS = 126
+PSC_NCHW, PSC_NHWC = 0, 1
+ACTIVATIONS = {"none": 0, "relu": 1, "silu": 2}
 
 STATUS_NAMES = {0: "PSC_OK", 1: "PSC_ERR_ARG", 2: "PSC_ERR_UNSUPPORTED", 3: "PSC_ERR_WORKSPACE",
                 4: "PSC_ERR_DEVICE", 5: "PSC_ERR_INTERNAL"}
@@ -45,6 +47,17 @@ class CConvConfig(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in (
         "kernel", "staged", "rows_per_lane", "cols_per_lane", "segments_per_wave", "column_tiles",
         "shares", "filters_per_block", "blocks", "threads_per_block")]
+
+
+class CParam(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("param", "grad", "copy", "m", "v", "scale")] + [
+        ("numel", ctypes.c_int64), ("weight_decay", ctypes.c_float), ("grad_dtype", ctypes.c_int32),
+        ("state_bits", ctypes.c_int32), ("reserved", ctypes.c_int32)]
+
+
+class CAdamW(ctypes.Structure):
+    _fields_ = [("lr", ctypes.c_float), ("beta1", ctypes.c_float), ("beta2", ctypes.c_float),
+                ("eps", ctypes.c_float), ("d_lr", ctypes.c_void_p)]
 
 
 PACKED_FIELDS = ("filter_perm", "filter_ptr", "seg_ptr", "cin_idx", "pat_id", "values")
@@ -116,6 +129,12 @@ def lib() -> ctypes.CDLL:
         "psc_dense3x3_fwd_workspace": ([i32, i32, i32, ctypes.POINTER(sz)], ctypes.c_int),
         "psc_dense3x3_fwd_ws": ([i32, P, i32, i32, i32, i32, P, i32, P, i32, P, P, sz, P], ctypes.c_int),
         "psc_maxpool2x2": ([i32, P, i32, i32, i32, i32, P, P], ctypes.c_int),
+        "psc_group_norm_workspace": ([i32] * 8 + [ctypes.POINTER(sz)], ctypes.c_int),
+        "psc_group_norm_fwd": ([i32, i32, P] + [i32] * 5 + [P, P, ctypes.c_float, i32, P, P, P, P, sz, P], ctypes.c_int),
+        "psc_group_norm_bwd": ([i32, i32, P, P] + [i32] * 5 + [P, P, P, P, i32, P, P, P, P, sz, P], ctypes.c_int),
+        "psc_grad_norm": ([P, i32, ctypes.c_float, ctypes.c_float, P, P, sz, P], ctypes.c_int),
+        "psc_adamw_step": ([P, i32, ctypes.POINTER(CAdamW), P, P, P], ctypes.c_int),
+        "psc_adamw_moments": ([P, P, P, i64, P, P, P], ctypes.c_int),
     }
     for name, (args, res) in sig.items():
         fn = getattr(L, name)
@@ -599,6 +618,296 @@ class AdmmLayer:
         admm_dual(self.layer, self.v, self.pat, self.keep_mask, self.a, self.d, stream)
         self.k += 1
         return self.loss
+
+
+# ------------------------------------------------------------------ group normalisation
+def _same_device(*tensors):
+    """The tensors of a call lie on the current device, whose streams it runs on."""
+    torch = _torch()
+    at = torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and t.device.index != at:
+            raise ValueError("a tensor lies on %s, and the current device is cuda:%d" % (t.device, at))
+
+
+def _layout(x) -> int:
+    """The layout of a 4-D device tensor [n, c, h, w] (of one that is in both, NCHW)."""
+    if x.dim() != 4 or not x.is_cuda:
+        raise ValueError("x must be a 4-D device tensor")
+    if x.is_contiguous():
+        return PSC_NCHW
+    if x.is_contiguous(memory_format=_torch().channels_last):
+        return PSC_NHWC
+    raise ValueError("x must be contiguous, in NCHW or with the channels last")
+
+
+def _like(t, x, layout, name):
+    """The address of ``t``, which has the shape, type and layout of ``x``."""
+    torch = _torch()
+    if t.dtype != x.dtype or t.shape != x.shape or not t.is_cuda or not t.is_contiguous(
+            memory_format=torch.channels_last if layout == PSC_NHWC else torch.contiguous_format):
+        raise ValueError("%s must have the shape, type and layout of x" % name)
+    return t.data_ptr() if t.numel() else None
+
+
+def _vector(t, numel, name):
+    if t is not None and t.numel() != numel:
+        raise ValueError("%s must have %d elements" % (name, numel))
+    return _f32(t, name)
+
+
+def _act_code(act) -> int:
+    if act not in ACTIVATIONS:
+        raise ValueError("act must be one of %s" % ", ".join(ACTIVATIONS))
+    return ACTIVATIONS[act]
+
+
+def group_norm_workspace(dtype: int, layout: int, n: int, c: int, h: int, w: int, groups: int,
+                         backward: bool = False) -> int:
+    """psc_group_norm_workspace: bytes of scratch (host only)."""
+    b = ctypes.c_size_t(0)
+    _check(lib().psc_group_norm_workspace(int(dtype), int(layout), int(n), int(c), int(h), int(w), int(groups),
+                                          int(bool(backward)), ctypes.byref(b)), "psc_group_norm_workspace")
+    return int(b.value)
+
+
+def _norm_scratch(ws, args, backward, stream):
+    """The address and size of ``ws``, or of scratch of this call's own."""
+    if ws is None:
+        need = group_norm_workspace(*args, backward)
+        ws = _scratch(need, stream) if need else None
+    return ws, _dev(ws, "ws"), _ws_bytes(ws)
+
+
+def group_norm_fwd(x, groups: int, gamma, beta, y, eps: float = 1e-5, act: str = "none", mean=None, rstd=None,
+                   ws=None, stream=None):
+    """psc_group_norm_fwd: y = act(gamma * xhat + beta) over ``groups`` groups
+    of channels of x [n, c, h, w], contiguous or channels_last (y the same);
+    gamma and beta (fp32, or None), and mean and rstd (fp32 [n, groups], or
+    None), which group_norm_bwd reads.  act: "none", "relu" or "silu"."""
+    layout, code, dt = _layout(x), _act_code(act), dtype_code(x)
+    n, c, h, w = x.shape
+    groups = int(groups)
+    _same_device(x, gamma, beta, y, mean, rstd, ws)
+    keep, wp, wb = _norm_scratch(ws, (dt, layout, n, c, h, w, groups), False, stream)
+    _check(lib().psc_group_norm_fwd(dt, layout, x.data_ptr() if n else None, n, c, h, w, groups,
+                                    _vector(gamma, c, "gamma"), _vector(beta, c, "beta"), float(eps), code,
+                                    _like(y, x, layout, "y"), _vector(mean, n * groups, "mean"),
+                                    _vector(rstd, n * groups, "rstd"), wp, wb, _stream(stream)), "psc_group_norm_fwd")
+
+
+def group_norm_bwd(x, dy, groups: int, gamma, beta, mean, rstd, dx, dgamma=None, dbeta=None, act: str = "none",
+                   ws=None, stream=None):
+    """psc_group_norm_bwd: dx, and dgamma and dbeta (fp32 [c], or None), from
+    the gradient dy of group_norm_fwd's output and the statistics that it
+    wrote; dy and dx have the type and layout of x."""
+    layout, code, dt = _layout(x), _act_code(act), dtype_code(x)
+    n, c, h, w = x.shape
+    groups = int(groups)
+    _same_device(x, dy, gamma, beta, mean, rstd, dx, dgamma, dbeta, ws)
+    keep, wp, wb = _norm_scratch(ws, (dt, layout, n, c, h, w, groups), True, stream)
+    _check(lib().psc_group_norm_bwd(dt, layout, x.data_ptr() if n else None, _like(dy, x, layout, "dy"), n, c, h, w,
+                                    groups, _vector(gamma, c, "gamma"), _vector(beta, c, "beta"),
+                                    _vector(mean, n * groups, "mean"), _vector(rstd, n * groups, "rstd"), code,
+                                    _like(dx, x, layout, "dx"), _vector(dgamma, c, "dgamma"),
+                                    _vector(dbeta, c, "dbeta"), wp, wb, _stream(stream)), "psc_group_norm_bwd")
+
+
+# ------------------------------------------------------------------ the optimiser
+GRAD_NORM_WS_BYTES = 8192
+ADAMW_STATE_BYTES = 64
+ADAMW_GROUP = 256           # elements that share the scales of 8-bit moments
+
+
+class ParamList:
+    """The tensors of grad_norm and adamw_step (an array of psc_param), which
+    it holds: ``grads`` (fp32 or fp16), and for the step ``params`` (fp32),
+    ``m`` and ``v`` (fp32, or int8 and uint8 codes with their ``scale``) and
+    ``copies`` (fp16, or None).  ``weight_decay`` is one value or one for each
+    tensor.  params None: a list for grad_norm alone."""
+
+    def __init__(self, params, grads, m=None, v=None, scale=None, copies=None, weight_decay=0.0):
+        torch = _torch()
+        grads = list(grads)
+        k = len(grads)
+        params, m, v, scale, copies = (list(t) if t is not None else [None] * k
+                                       for t in (params, m, v, scale, copies))
+        decay = list(weight_decay) if hasattr(weight_decay, "__len__") else [weight_decay] * k
+        if not all(len(t) == k for t in (params, m, v, scale, copies, decay)):
+            raise ValueError("every list must have one entry for each gradient")
+        self.c = (CParam * max(k, 1))()
+        self.count, self.device = k, grads[0].device if k else None
+        self._held = (params, m, v, scale, copies)
+        read, written = [], []
+        for i in range(k):
+            e, p, n = self.c[i], params[i], int(grads[i].numel())
+            e.numel, e.weight_decay, e.state_bits = n, float(decay[i]), 32
+            if p is None:
+                continue
+            bits8 = m[i] is not None and m[i].dtype == torch.int8
+            e.state_bits = 8 if bits8 else 32
+            want = {"params": (p, torch.float32, n), "m": (m[i], torch.int8 if bits8 else torch.float32, n),
+                    "v": (v[i], torch.uint8 if bits8 else torch.float32, n)}
+            if bits8:
+                want["scale"] = (scale[i], torch.float32, 2 * -(-n // ADAMW_GROUP))
+            if copies[i] is not None:
+                want["copies"] = (copies[i], torch.float16, n)
+            for name, (t, dt, size) in want.items():
+                if t is None or t.dtype != dt or t.numel() != size:
+                    raise ValueError("%s[%d] must be a tensor of %d elements of %s" % (name, i, size, dt))
+                if t.device != grads[i].device:
+                    raise ValueError("%s[%d] and its gradient lie on different devices" % (name, i))
+            e.param, e.m, e.v, e.scale, e.copy = (_dev(t, "params, m, v, scale and copies") for t in (
+                p, m[i], v[i], scale[i] if bits8 else None, copies[i]))
+            written += [(t.data_ptr(), t.data_ptr() + t.numel() * t.element_size())
+                        for t, _, _ in want.values() if t.numel()]
+        written.sort()
+        self._written = written
+        if any(a[1] > b[0] for a, b in zip(written, written[1:])):
+            raise ValueError("tensors that the step writes overlap (the same one twice in the list?)")
+        self.set_grads(grads)
+
+    def set_grads(self, grads):
+        """Other gradients in the place of the present ones."""
+        grads = list(grads)
+        if len(grads) != self.count:
+            raise ValueError("there must be one gradient for each tensor")
+        import bisect
+        for i, g in enumerate(grads):
+            if g.numel() != self.c[i].numel or g.device != self.device:
+                raise ValueError("grads[%d] must have %d elements on %s" % (i, self.c[i].numel, self.device))
+            a, b = g.data_ptr(), g.data_ptr() + g.numel() * g.element_size()
+            at = bisect.bisect_left(self._written, (b, 0))
+            if g.numel() and at and self._written[at - 1][1] > a:
+                raise ValueError("grads[%d] overlaps a tensor that the step writes" % i)
+        codes = [dtype_code(g) for g in grads]
+        addresses = [_dev(g, "grads") for g in grads]
+        for i in range(self.count):
+            self.c[i].grad, self.c[i].grad_dtype = addresses[i], codes[i]
+        self.grads = grads
+
+    def check_device(self):
+        if self.count:
+            _same_device(self.grads[0])
+
+
+def grad_norm(params: ParamList, out, max_norm: float = float("inf"), scale: float = 1.0, ws=None, stream=None):
+    """psc_grad_norm: out (fp32 [2], device) = the norm of all gradients times
+    ``scale``, and the factor that unscales and clips them to ``max_norm``
+    (NaN if the norm is not finite)."""
+    params.check_device()
+    _same_device(out, ws)
+    if out.numel() != 2:
+        raise ValueError("out must have 2 elements")
+    if ws is None:
+        ws = _scratch(GRAD_NORM_WS_BYTES, stream)
+    _check(lib().psc_grad_norm(params.c, params.count, float(scale), float(max_norm), _f32(out, "out"), _dev(ws, "ws"),
+                               _ws_bytes(ws), _stream(stream)), "psc_grad_norm")
+
+
+def adamw_step(params: ParamList, state, lr, betas=(0.9, 0.999), eps: float = 1e-8, factor=None, stream=None):
+    """psc_adamw_step: one step on every tensor of the list.  ``state``: a
+    device tensor of 64 bytes, zeros before the first step; ``lr``: a number,
+    or an fp32 device tensor that the step reads; ``factor``: None, or an fp32
+    device tensor whose first element the gradients are multiplied by."""
+    params.check_device()
+    on_device = hasattr(lr, "data_ptr")
+    _same_device(state, factor, lr if on_device else None)
+    for t, name in ((factor, "factor"), (lr if on_device else None, "lr")):
+        if t is not None and t.numel() < 1:
+            raise ValueError("%s must have an element" % name)
+    if _ws_bytes(state) < ADAMW_STATE_BYTES:
+        raise ValueError("state must have %d bytes" % ADAMW_STATE_BYTES)
+    opt = CAdamW(0.0 if on_device else float(lr), float(betas[0]), float(betas[1]), float(eps),
+                 _f32(lr, "lr") if on_device else None)
+    _check(lib().psc_adamw_step(params.c, params.count, ctypes.byref(opt), _f32(factor, "factor"), _dev(state, "state"),
+                                _stream(stream)), "psc_adamw_step")
+
+
+def adamw_moments(m, v, scale, m_out, v_out, stream=None):
+    """psc_adamw_moments: the values (fp32) that 8-bit moments stand for."""
+    torch = _torch()
+    n = int(m.numel())
+    if m.dtype != torch.int8 or v.dtype != torch.uint8 or v.numel() != n or \
+            scale.numel() != 2 * -(-n // ADAMW_GROUP) or m_out.numel() != n or v_out.numel() != n:
+        raise ValueError("m, v, scale, m_out and v_out do not go together")
+    _same_device(m, v, scale, m_out, v_out)
+    _check(lib().psc_adamw_moments(_dev(m, "m"), _dev(v, "v"), _f32(scale, "scale"), n, _f32(m_out, "m_out"),
+                                   _f32(v_out, "v_out"), _stream(stream)), "psc_adamw_moments")
+
+
+class AdamW:
+    """The optimiser of a list of fp32 device tensors (``params``) and their
+    gradients' buffers: the moments (``m`` and ``v``, flat, each tensor's at a
+    multiple of 256 elements; with state_bits 8 codes, and their ``scale``),
+    the count of ``steps`` done (an int64 device tensor), and the gradient
+    ``norm`` with its clip ``factor``.  lr: a number, or an fp32 device tensor
+    that each step reads (also one replayed from a graph)."""
+
+    def __init__(self, params, grads, lr=1e-3, betas=(0.9, 0.999), eps: float = 1e-8, weight_decay=0.0,
+                 state_bits: int = 32, copies=None):
+        torch = _torch()
+        if state_bits not in (8, 32):
+            raise ValueError("state_bits must be 8 or 32")
+        params = list(params)
+        if not params:
+            raise ValueError("there must be a tensor to optimise")
+        self.lr, self.betas, self.eps = lr, tuple(betas), float(eps)
+        device = params[0].device
+        at, total = [], 0
+        for p in params:
+            at.append(total)
+            total += -(-int(p.numel()) // ADAMW_GROUP) * ADAMW_GROUP
+        bits8 = state_bits == 8
+        self.m = torch.zeros(total, dtype=torch.int8 if bits8 else torch.float32, device=device)
+        self.v = torch.zeros(total, dtype=torch.uint8 if bits8 else torch.float32, device=device)
+        self.scale = torch.zeros((total // ADAMW_GROUP, 2), dtype=torch.float32, device=device) if bits8 else None
+        each = lambda flat: [flat[a:a + p.numel()] for a, p in zip(at, params)]                     # noqa: E731
+        scales = [self.scale[a // ADAMW_GROUP:a // ADAMW_GROUP - (-p.numel() // ADAMW_GROUP)]
+                  for a, p in zip(at, params)] if bits8 else None
+        self.params = ParamList(params, grads, each(self.m), each(self.v), scales, copies, weight_decay)
+        self._state = torch.zeros(ADAMW_STATE_BYTES // 8, dtype=torch.int64, device=device)
+        self.steps = self._state[:1]
+        self._out = torch.zeros(2, dtype=torch.float32, device=device)
+        self.norm, self.factor = self._out[:1], self._out[1:]
+        self._ws = torch.empty(GRAD_NORM_WS_BYTES, dtype=torch.uint8, device=device)
+
+    def _hold(self, stream):
+        """Work on another stream than the one that the memory came from: it is
+        not given out again before that is done."""
+        if stream is not None:
+            s = _torch_stream(stream)
+            for t in (self.m, self.v, self.scale, self._state, self._out, self._ws):
+                if t is not None:
+                    t.record_stream(s)
+
+    def grad_norm(self, max_norm: float = float("inf"), scale: float = 1.0, stream=None):
+        """The norm of the gradients and the factor that clips them, which
+        step(factor=self.factor) applies: [norm, factor] on the device."""
+        self._hold(stream)
+        grad_norm(self.params, self._out, max_norm, scale, self._ws, stream)
+        return self._out
+
+    def step(self, factor=None, stream=None):
+        """One step on every tensor (none if ``factor`` is not finite)."""
+        self._hold(stream)
+        adamw_step(self.params, self._state, self.lr, self.betas, self.eps, factor, stream)
+
+    def moments(self, stream=None):
+        """m and v as fp32 values, flat: the buffers themselves, or with 8 bits
+        what their codes stand for."""
+        if self.scale is None:
+            return self.m, self.v
+        torch = _torch()
+        with torch.cuda.stream(_torch_stream(stream)):
+            m, v = (torch.empty(self.m.numel(), dtype=torch.float32, device=self.m.device) for _ in range(2))
+        self._hold(stream)
+        most = 1 << 30
+        for a in range(0, self.m.numel(), most):
+            b = min(a + most, self.m.numel())
+            adamw_moments(self.m[a:b], self.v[a:b], self.scale[a // ADAMW_GROUP:-(-b // ADAMW_GROUP)], m[a:b], v[a:b],
+                          stream)
+        return m, v
 
 
 # ------------------------------------------------------------------ conveniences

@@ -145,4 +145,46 @@ bool conv_split_takes(const PatTable& tab, const ConvArgs& a);
 hipError_t launch_maxpool(int dtype, const void* x, int n, int c, int h, int w, void* y,
                           hipStream_t stream);
 
+
+// Group normalisation with an activation (act: PSC_ACT_*), NCHW or channels last.
+struct GroupNormArgs {
+    int dtype, channels_last;
+    int n, c, h, w, groups;
+    int act;
+};
+size_t group_norm_workspace_bytes(const GroupNormArgs& a, bool backward);
+hipError_t launch_group_norm_fwd(const GroupNormArgs& a, const void* x, const float* gamma, const float* beta, float eps,
+                                 void* y, float* mean, float* rstd, void* ws, hipStream_t stream);
+hipError_t launch_group_norm_bwd(const GroupNormArgs& a, const void* x, const void* dy, const float* gamma,
+                                 const float* beta, const float* mean, const float* rstd, void* dx, float* dgamma,
+                                 float* dbeta, void* ws, hipStream_t stream);
+
+// The optimiser: a tensor of its lists (psc_param), the gradient norm, the
+// AdamW step, and 8-bit moments as the values they stand for.
+struct ParamView {
+    float* param;
+    const void* grad;
+    void* copy;
+    void* m;
+    void* v;
+    float* scale;
+    int64_t numel;
+    float weight_decay;
+    int32_t grad_dtype;
+    int32_t state_bits;
+    int32_t reserved;
+};
+struct AdamwArgs {
+    float lr, beta1, beta2, eps;
+    const float* d_lr;
+};
+constexpr size_t kAdamwStateBytes = 64;
+size_t grad_norm_workspace_bytes();
+hipError_t launch_grad_norm(const ParamView* q, int count, float scale, float max_norm, float* out, void* ws,
+                            hipStream_t stream);
+hipError_t launch_adamw(const ParamView* q, int count, const AdamwArgs& a, const float* factor, void* state,
+                        hipStream_t stream);
+hipError_t launch_moments(const int8_t* qm, const uint8_t* qv, const float* scale, int64_t numel, float* m, float* v,
+                          hipStream_t stream);
+
 }  // namespace psc

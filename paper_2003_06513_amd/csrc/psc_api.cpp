@@ -6,7 +6,9 @@
 #include <cmath>
 #include <cstdarg>
 #include <cstdio>
+#include <cstddef>
 #include <cstring>
+#include <limits>
 #include <string>
 
 #include "../../include/psc.h"
@@ -546,6 +548,152 @@ psc_status psc_admm_dual(const psc_layer* L, const float* d_v, const uint8_t* d_
     return device_status(psc::launch_admm_dual(t, d_v, d_pat, d_keep, int64_t(L->cout) * L->cin, d_a, d_d,
                                                as_stream(stream)),
                          "psc_admm_dual launch");
+}
+
+// ---- group normalisation
+
+static psc_status check_group_norm(int32_t dtype, int32_t layout, int32_t n, int32_t c, int32_t h, int32_t w,
+                                   int32_t groups, int32_t act, psc::GroupNormArgs* a) {
+    if (!dtype_ok(dtype)) return fail(PSC_ERR_ARG, "dtype=%d is not a psc_dtype", dtype);
+    if (layout != PSC_NCHW && layout != PSC_NHWC) return fail(PSC_ERR_ARG, "layout=%d is not a psc_layout", layout);
+    if (n < 0 || n > 65535 || c < 1 || c > 65535 || h < 1 || w < 1 || h > 32768 || w > 32768)
+        return fail(PSC_ERR_ARG, "bad shape n=%d c=%d h=%d w=%d", n, c, h, w);
+    const int64_t plane = int64_t(h) * w;
+    if (c * plane > kMaxElems || n * (c * plane) > kMaxElems)
+        return fail(PSC_ERR_ARG, "a tensor holds more than 2^31-1 elements");
+    if (groups < 1 || groups > c || c % groups) return fail(PSC_ERR_ARG, "groups=%d does not divide c=%d", groups, c);
+    if (act < PSC_ACT_NONE || act > PSC_ACT_SILU) return fail(PSC_ERR_ARG, "act=%d is not a psc_act", act);
+    *a = psc::GroupNormArgs{dtype, layout == PSC_NHWC, n, c, h, w, groups, act};
+    return PSC_OK;
+}
+
+static psc_status check_ws(const char* what, size_t need, const void* d_ws, size_t ws_bytes) {
+    if (need && (!d_ws || ws_bytes < need))
+        return fail(PSC_ERR_WORKSPACE, "%s needs %zu workspace bytes, got %zu", what, need, d_ws ? ws_bytes : size_t(0));
+    if (need && (reinterpret_cast<uintptr_t>(d_ws) & 255u))
+        return fail(PSC_ERR_WORKSPACE, "workspace must be 256-byte aligned");
+    return PSC_OK;
+}
+
+psc_status psc_group_norm_workspace(int32_t dtype, int32_t layout, int32_t n, int32_t c, int32_t h, int32_t w,
+                                    int32_t groups, int32_t backward, size_t* bytes) {
+    psc::GroupNormArgs a;
+    if (psc_status s = check_group_norm(dtype, layout, n, c, h, w, groups, PSC_ACT_NONE, &a)) return s;
+    if (!bytes) return fail(PSC_ERR_ARG, "bytes is NULL");
+    *bytes = psc::group_norm_workspace_bytes(a, backward != 0);
+    return ok();
+}
+
+psc_status psc_group_norm_fwd(int32_t dtype, int32_t layout, const void* d_x, int32_t n, int32_t c, int32_t h,
+                              int32_t w, int32_t groups, const float* d_gamma, const float* d_beta, float eps,
+                              int32_t act, void* d_y, float* d_mean, float* d_rstd, void* d_ws, size_t ws_bytes,
+                              void* stream) {
+    psc::GroupNormArgs a;
+    if (psc_status s = check_group_norm(dtype, layout, n, c, h, w, groups, act, &a)) return s;
+    if (!(eps > 0.f) || !std::isfinite(eps)) return fail(PSC_ERR_ARG, "eps must be positive and finite");
+    if (!d_mean != !d_rstd) return fail(PSC_ERR_ARG, "d_mean and d_rstd must be both NULL or both non-NULL");
+    if (n == 0) return ok();
+    if (!d_x || !d_y) return fail(PSC_ERR_ARG, "d_x and d_y must be non-NULL");
+    const size_t bytes = size_t(int64_t(n) * c * h * w) * elt_size(dtype);
+    if (overlaps(d_x, bytes, d_y, bytes)) return fail(PSC_ERR_ARG, "d_y overlaps d_x");
+    if (psc_status s = check_ws("psc_group_norm_fwd", psc::group_norm_workspace_bytes(a, false), d_ws, ws_bytes))
+        return s;
+    return device_status(psc::launch_group_norm_fwd(a, d_x, d_gamma, d_beta, eps, d_y, d_mean, d_rstd, d_ws,
+                                                    as_stream(stream)),
+                         "psc_group_norm_fwd launch");
+}
+
+psc_status psc_group_norm_bwd(int32_t dtype, int32_t layout, const void* d_x, const void* d_dy, int32_t n, int32_t c,
+                              int32_t h, int32_t w, int32_t groups, const float* d_gamma, const float* d_beta,
+                              const float* d_mean, const float* d_rstd, int32_t act, void* d_dx, float* d_dgamma,
+                              float* d_dbeta, void* d_ws, size_t ws_bytes, void* stream) {
+    psc::GroupNormArgs a;
+    if (psc_status s = check_group_norm(dtype, layout, n, c, h, w, groups, act, &a)) return s;
+    if (n > 0 && (!d_x || !d_dy || !d_dx || !d_mean || !d_rstd))
+        return fail(PSC_ERR_ARG, "d_x, d_dy, d_dx, d_mean and d_rstd must be non-NULL");
+    const size_t bytes = size_t(int64_t(n) * c * h * w) * elt_size(dtype);
+    if (overlaps(d_x, bytes, d_dx, bytes) || overlaps(d_dy, bytes, d_dx, bytes))
+        return fail(PSC_ERR_ARG, "d_dx overlaps d_x or d_dy");
+    if (psc_status s = check_ws("psc_group_norm_bwd", psc::group_norm_workspace_bytes(a, true), d_ws, ws_bytes))
+        return s;
+    return device_status(psc::launch_group_norm_bwd(a, d_x, d_dy, d_gamma, d_beta, d_mean, d_rstd, d_dx, d_dgamma,
+                                                    d_dbeta, d_ws, as_stream(stream)),
+                         "psc_group_norm_bwd launch");
+}
+
+// ---- the optimiser.  A psc_param is what the launchers take.
+
+static_assert(sizeof(psc_param) == sizeof(psc::ParamView) && offsetof(psc_param, scale) == offsetof(psc::ParamView, scale) &&
+                  offsetof(psc_param, state_bits) == offsetof(psc::ParamView, state_bits),
+              "one layout");
+static_assert(PSC_ADAMW_STATE_BYTES == psc::kAdamwStateBytes, "one size");
+
+static psc_status check_params(const psc_param* q, int32_t count, bool step) {
+    if (count < 0) return fail(PSC_ERR_ARG, "count=%d < 0", count);
+    if (count > 0 && !q) return fail(PSC_ERR_ARG, "h_params is NULL");
+    for (int32_t i = 0; i < count; ++i) {
+        if (q[i].numel < 0 || q[i].numel > kMaxElems)
+            return fail(PSC_ERR_ARG, "params[%d]: numel=%lld outside 0..2^31-1", i, (long long)q[i].numel);
+        if (!dtype_ok(q[i].grad_dtype)) return fail(PSC_ERR_ARG, "params[%d]: grad_dtype=%d is not a psc_dtype", i, q[i].grad_dtype);
+        if (q[i].numel > 0 && !q[i].grad) return fail(PSC_ERR_ARG, "params[%d]: grad is NULL", i);
+        if (reinterpret_cast<uintptr_t>(q[i].grad) % elt_size(q[i].grad_dtype))
+            return fail(PSC_ERR_ARG, "params[%d]: grad is not aligned to its elements", i);
+        if (!step) continue;
+        if (q[i].state_bits != 32 && q[i].state_bits != 8)
+            return fail(PSC_ERR_ARG, "params[%d]: state_bits=%d is neither 32 nor 8", i, q[i].state_bits);
+        if (q[i].reserved) return fail(PSC_ERR_ARG, "params[%d]: reserved must be 0", i);
+        if (!(q[i].weight_decay >= 0.f) || !std::isfinite(q[i].weight_decay))
+            return fail(PSC_ERR_ARG, "params[%d]: weight_decay must be finite and >= 0", i);
+        if (q[i].numel == 0) continue;
+        if (!q[i].param || !q[i].m || !q[i].v) return fail(PSC_ERR_ARG, "params[%d]: param, m and v must be non-NULL", i);
+        if (q[i].state_bits == 8 && (!q[i].scale || (reinterpret_cast<uintptr_t>(q[i].scale) & 7u)))
+            return fail(PSC_ERR_ARG, "params[%d]: scale must be non-NULL and 8-byte aligned", i);
+        const uintptr_t four = reinterpret_cast<uintptr_t>(q[i].param) |
+                               (q[i].state_bits == 32 ? reinterpret_cast<uintptr_t>(q[i].m) | reinterpret_cast<uintptr_t>(q[i].v) : 0);
+        if ((four & 3u) || (reinterpret_cast<uintptr_t>(q[i].copy) & 1u))
+            return fail(PSC_ERR_ARG, "params[%d]: a tensor is not aligned to its elements", i);
+    }
+    return PSC_OK;
+}
+
+psc_status psc_grad_norm(const psc_param* h_params, int32_t count, float scale, float max_norm, float* d_out, void* d_ws,
+                         size_t ws_bytes, void* stream) {
+    if (psc_status s = check_params(h_params, count, false)) return s;
+    if (!(scale > 0.f) || !std::isfinite(scale)) return fail(PSC_ERR_ARG, "scale must be positive and finite");
+    if (!(max_norm > 0.f)) return fail(PSC_ERR_ARG, "max_norm must be positive");
+    if (!d_out) return fail(PSC_ERR_ARG, "d_out is NULL");
+    if (psc_status s = check_ws("psc_grad_norm", psc::grad_norm_workspace_bytes(), d_ws, ws_bytes)) return s;
+    return device_status(psc::launch_grad_norm(reinterpret_cast<const psc::ParamView*>(h_params), count, scale, max_norm,
+                                               d_out, d_ws, as_stream(stream)),
+                         "psc_grad_norm launch");
+}
+
+psc_status psc_adamw_step(const psc_param* h_params, int32_t count, const psc_adamw* opt, const float* d_factor,
+                          void* d_state, void* stream) {
+    if (psc_status s = check_params(h_params, count, true)) return s;
+    if (!opt) return fail(PSC_ERR_ARG, "opt is NULL");
+    if (!std::isfinite(opt->lr)) return fail(PSC_ERR_ARG, "lr must be finite");
+    if (!(opt->beta1 >= 0.f && opt->beta1 < 1.f && opt->beta2 >= 0.f && opt->beta2 < 1.f))
+        return fail(PSC_ERR_ARG, "beta1 and beta2 must lie in [0, 1)");
+    if (!(opt->eps >= std::numeric_limits<float>::min()) || !std::isfinite(opt->eps))
+        return fail(PSC_ERR_ARG, "eps must be finite and at least FLT_MIN");
+    if (!d_state || (reinterpret_cast<uintptr_t>(d_state) & 255u))
+        return fail(PSC_ERR_ARG, "d_state must be non-NULL and 256-byte aligned");
+    const psc::AdamwArgs a{opt->lr, opt->beta1, opt->beta2, opt->eps, opt->d_lr};
+    return device_status(psc::launch_adamw(reinterpret_cast<const psc::ParamView*>(h_params), count, a, d_factor, d_state,
+                                           as_stream(stream)),
+                         "psc_adamw_step launch");
+}
+
+psc_status psc_adamw_moments(const void* d_m, const void* d_v, const float* d_scale, int64_t numel, float* d_m_out,
+                             float* d_v_out, void* stream) {
+    if (numel < 0 || numel > kMaxElems) return fail(PSC_ERR_ARG, "numel=%lld outside 0..2^31-1", (long long)numel);
+    if (numel == 0) return ok();
+    if (!d_m || !d_v || !d_scale || !d_m_out || !d_v_out) return fail(PSC_ERR_ARG, "every pointer must be non-NULL");
+    if (reinterpret_cast<uintptr_t>(d_scale) & 7u) return fail(PSC_ERR_ARG, "d_scale must be 8-byte aligned");
+    return device_status(psc::launch_moments(static_cast<const int8_t*>(d_m), static_cast<const uint8_t*>(d_v), d_scale,
+                                             numel, d_m_out, d_v_out, as_stream(stream)),
+                         "psc_adamw_moments launch");
 }
 
 psc_status psc_dense3x3_fwd_ws(int32_t dtype, const void* d_x, int32_t n, int32_t cin, int32_t h,
