@@ -1,224 +1,275 @@
-// Group normalisation with an activation, forward and backward, for
-// activations in NCHW or with the channels last.
-//
-// For image n and group g of Cg = C / G channels, over its M = Cg H W values:
-//   mu = mean x,  r = 1 / sqrt(var x + eps),  xh = (x - mu) r
-//   y  = act(u),  u = gamma[c] xh + beta[c]
-// and for the gradient dy of y, with du = dy act'(u):
-//   A[n,c] = sum du,  B[n,c] = sum du xh        (over H W)
-//   dbeta = sum_n A,  dgamma = sum_n B
-//   dx = r (gamma du - (S1 + xh S2) / M),  S1 = sum_c gamma A,  S2 = sum_c gamma B
-// Everything is summed in fp32, the variance about the mean.
-#include "common.h"
-#include "launch.h"
+// Group normalisation: how a call runs, and the sums between the passes over
+// pieces.
+#include "group_norm.h"
 
 namespace psc {
+namespace gn {
 namespace {
 
-enum : int { ACT_NONE = 0, ACT_RELU = 1, ACT_SILU = 2 };
-
-__device__ __forceinline__ float sigmoid(float u) { return __builtin_amdgcn_rcpf(1.f + __expf(-u)); }
-__device__ __forceinline__ float act_of(float u, int act) {
-    return act == ACT_RELU ? (u < 0.f ? 0.f : u) : act == ACT_SILU ? u * sigmoid(u) : u;
-}
-// u rounds after the product and after the sum, in the forward and in the
-// backward: the ReLU passes the gradient of exactly the outputs above zero.
-__device__ __forceinline__ float affine(float xh, float ga, float be) {
-#pragma clang fp contract(off)
-    return xh * ga + be;
-}
-// The gradient at u of a gradient dy at act(u).
-__device__ __forceinline__ float act_back(float u, float dy, int act) {
-    if (act == ACT_RELU) return u > 0.f ? dy : 0.f;
-    if (act == ACT_SILU) {
-        const float s = sigmoid(u);
-        return dy * (s * fmaf(u, 1.f - s, 1.f));
+// The statistics of a group from its pieces: the means weighted by their
+// counts, the squares about the common mean.
+__global__ __launch_bounds__(256) void k_gn_combine_fwd(const float4* __restrict__ parts, int per, float eps,
+                                                        float* __restrict__ mean, float* __restrict__ rstd) {
+    __shared__ float part[16];
+    const float4* p = parts + int64_t(blockIdx.x) * per;
+    float sum = 0.f, num = 0.f;
+    for (int i = threadIdx.x; i < per; i += 256) {
+        sum = fmaf(p[i].z, p[i].x, sum);
+        num += p[i].z;
     }
-    return dy;
-}
-
-__device__ __forceinline__ float block_sum(float x, float* part) {
-#pragma unroll
-    for (int off = 32; off > 0; off >>= 1) x += __shfl_xor(x, off);
-    __syncthreads();
-    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = x;
-    __syncthreads();
-    return (part[0] + part[1]) + (part[2] + part[3]);
-}
-
-// Where element j of group (n, g), or pixel s of channel c, lies.
-struct Shape {
-    int c, cg, groups;
-    int64_t hw;
-    int64_t sc, ss;      // strides of a channel and of a pixel
-};
-
-template <int DT>
-__global__ __launch_bounds__(256) void k_gn_stats(const typename Elt<DT>::T* __restrict__ x, Shape s, float eps,
-                                                  float* __restrict__ mean, float* __restrict__ rstd) {
-    __shared__ float part[4];
-    const int64_t n = blockIdx.x / s.groups;
-    const int g = int(blockIdx.x % s.groups);
-    const typename Elt<DT>::T* p = x + n * s.c * s.hw + int64_t(g) * s.cg * s.sc;
-    float sum = 0.f;
-    for (int c = 0; c < s.cg; ++c)
-        for (int64_t i = threadIdx.x; i < s.hw; i += 256) sum += Elt<DT>::load(p, c * s.sc + i * s.ss);
-    const float m = float(s.cg) * float(s.hw);
-    const float mu = block_sum(sum, part) / m;
+    num = block_sum(num, part);
+    const float mu = block_sum(sum, part) / num;
     float sq = 0.f;
-    for (int c = 0; c < s.cg; ++c)
-        for (int64_t i = threadIdx.x; i < s.hw; i += 256) {
-            const float d = Elt<DT>::load(p, c * s.sc + i * s.ss) - mu;
-            sq = fmaf(d, d, sq);
-        }
+    for (int i = threadIdx.x; i < per; i += 256) {
+        const float d = p[i].x - mu;
+        sq += fmaf(p[i].z * d, d, p[i].y);
+    }
     sq = block_sum(sq, part);
     if (threadIdx.x == 0) {
         mean[blockIdx.x] = mu;
-        rstd[blockIdx.x] = 1.f / sqrtf(sq / m + eps);
+        rstd[blockIdx.x] = 1.f / sqrtf(sq / num + eps);
     }
 }
 
-// One channel of one image per block.
-template <int DT>
-__global__ __launch_bounds__(256) void k_gn_apply(const typename Elt<DT>::T* __restrict__ x, Shape s,
-                                                  const float* __restrict__ gamma, const float* __restrict__ beta,
-                                                  const float* __restrict__ mean, const float* __restrict__ rstd,
-                                                  int act, typename Elt<DT>::T* __restrict__ y) {
-    const int64_t n = blockIdx.x / s.c;
-    const int c = int(blockIdx.x % s.c);
-    const int64_t at = n * s.c * s.hw + c * s.sc, g = n * s.groups + c / s.cg;
-    const float mu = mean[g], r = rstd[g], ga = gamma ? gamma[c] : 1.f, be = beta ? beta[c] : 0.f;
-    for (int64_t i = threadIdx.x; i < s.hw; i += 256)
-        y[at + i * s.ss] = Elt<DT>::from_f(act_of(affine((Elt<DT>::load(x, at + i * s.ss) - mu) * r, ga, be), act));
-}
-
-template <int DT>
-__global__ __launch_bounds__(256) void k_gn_sums(const typename Elt<DT>::T* __restrict__ x,
-                                                 const typename Elt<DT>::T* __restrict__ dy, Shape s,
-                                                 const float* __restrict__ gamma, const float* __restrict__ beta,
-                                                 const float* __restrict__ mean, const float* __restrict__ rstd,
-                                                 int act, float2* __restrict__ sums) {
-    __shared__ float part[4];
-    const int64_t n = blockIdx.x / s.c;
-    const int c = int(blockIdx.x % s.c);
-    const int64_t at = n * s.c * s.hw + c * s.sc, g = n * s.groups + c / s.cg;
-    const float mu = mean[g], r = rstd[g], ga = gamma ? gamma[c] : 1.f, be = beta ? beta[c] : 0.f;
-    float a = 0.f, b = 0.f;
-    for (int64_t i = threadIdx.x; i < s.hw; i += 256) {
-        const float xh = (Elt<DT>::load(x, at + i * s.ss) - mu) * r;
-        const float du = act_back(affine(xh, ga, be), Elt<DT>::load(dy, at + i * s.ss), act);
-        a += du;
-        b = fmaf(du, xh, b);
-    }
-    a = block_sum(a, part);
-    b = block_sum(b, part);
-    if (threadIdx.x == 0) sums[blockIdx.x] = make_float2(a, b);
-}
-
-template <int DT>
-__global__ __launch_bounds__(256) void k_gn_dx(const typename Elt<DT>::T* __restrict__ x,
-                                               const typename Elt<DT>::T* __restrict__ dy, Shape s,
-                                               const float* __restrict__ gamma, const float* __restrict__ beta,
-                                               const float* __restrict__ mean, const float* __restrict__ rstd, int act,
-                                               const float2* __restrict__ sums, typename Elt<DT>::T* __restrict__ dx) {
-    __shared__ float part[4];
-    const int64_t n = blockIdx.x / s.c;
-    const int c = int(blockIdx.x % s.c), g0 = c / s.cg * s.cg;
-    const int64_t at = n * s.c * s.hw + c * s.sc, g = n * s.groups + c / s.cg;
-    const float mu = mean[g], r = rstd[g], ga = gamma ? gamma[c] : 1.f, be = beta ? beta[c] : 0.f;
+__global__ __launch_bounds__(256) void k_gn_combine_bwd(const float2* __restrict__ parts, int per, int pieces,
+                                                        int groups, int cg, float m, const float* __restrict__ gamma,
+                                                        float2* __restrict__ s12) {
+    __shared__ float part[16];
+    const float2* p = parts + int64_t(blockIdx.x) * per;
+    const int c0 = int(blockIdx.x % unsigned(groups)) * cg;
     float s1 = 0.f, s2 = 0.f;
-    for (int k = threadIdx.x; k < s.cg; k += 256) {
-        const float2 ab = sums[n * s.c + g0 + k];
-        const float gk = gamma ? gamma[g0 + k] : 1.f;
-        s1 = fmaf(gk, ab.x, s1);
-        s2 = fmaf(gk, ab.y, s2);
+    for (int i = threadIdx.x; i < per; i += 256) {
+        const float ga = or_one(gamma, c0 + i / pieces);
+        s1 = fmaf(ga, p[i].x, s1);
+        s2 = fmaf(ga, p[i].y, s2);
     }
-    const float m = float(s.cg) * float(s.hw);
-    s1 = block_sum(s1, part) / m;
-    s2 = block_sum(s2, part) / m;
-    for (int64_t i = threadIdx.x; i < s.hw; i += 256) {
-        const float xh = (Elt<DT>::load(x, at + i * s.ss) - mu) * r;
-        const float du = act_back(affine(xh, ga, be), Elt<DT>::load(dy, at + i * s.ss), act);
-        dx[at + i * s.ss] = Elt<DT>::from_f(r * (fmaf(ga, du, -s1) - xh * s2));
-    }
+    s1 = block_sum(s1, part);
+    s2 = block_sum(s2, part);
+    if (threadIdx.x == 0) s12[blockIdx.x] = make_float2(s1 / m, s2 / m);
 }
 
-// dbeta and dgamma: the sums of a channel over the images, in their order.
-__global__ __launch_bounds__(256) void k_gn_param(const float2* __restrict__ sums, int n, int c,
-                                                  float* __restrict__ dgamma, float* __restrict__ dbeta) {
-    const int k = blockIdx.x * 256 + threadIdx.x;
-    if (k >= c) return;
+// dbeta and dgamma: a block adds 32 channels, each over the images' and
+// pieces' sums, 32 of them at a time, in a fixed order.
+__global__ __launch_bounds__(1024) void k_gn_param(const float2* __restrict__ sums, int n, int c, int pieces,
+                                                   float* __restrict__ dgamma, float* __restrict__ dbeta) {
+    __shared__ float2 part[32][33];
+    const int k = int(blockIdx.x) * 32 + int(threadIdx.x & 31), row = int(threadIdx.x >> 5);
     float a = 0.f, b = 0.f;
-    for (int i = 0; i < n; ++i) {
-        const float2 ab = sums[int64_t(i) * c + k];
-        a += ab.x;
-        b += ab.y;
+    if (k < c) {
+        const int64_t count = int64_t(n) * pieces;
+        for (int64_t i = row; i < count; i += 32) {
+            const int64_t img = i / pieces, piece = i - img * pieces;
+            const float2 ab = sums[(img * c + k) * pieces + piece];
+            a += ab.x;
+            b += ab.y;
+        }
     }
-    if (dgamma) dgamma[k] = b;
-    if (dbeta) dbeta[k] = a;
-}
-
-Shape shape_of(const GroupNormArgs& a) {
-    Shape s;
-    s.c = a.c, s.groups = a.groups, s.cg = a.c / a.groups;
-    s.hw = int64_t(a.h) * a.w;
-    s.sc = a.channels_last ? 1 : s.hw;
-    s.ss = a.channels_last ? a.c : 1;
-    return s;
-}
-
-template <int DT>
-hipError_t fwd(const GroupNormArgs& a, const void* x, const float* gamma, const float* beta, float eps, void* y,
-               float* mean, float* rstd, void* ws, hipStream_t stream) {
-    using T = typename Elt<DT>::T;
-    const Shape s = shape_of(a);
-    const int64_t ng = int64_t(a.n) * a.groups;
-    if (!mean) mean = static_cast<float*>(ws), rstd = mean + ng;
-    hipLaunchKernelGGL((k_gn_stats<DT>), dim3(unsigned(ng)), dim3(256), 0, stream, static_cast<const T*>(x), s, eps,
-                       mean, rstd);
-    hipLaunchKernelGGL((k_gn_apply<DT>), dim3(unsigned(int64_t(a.n) * a.c)), dim3(256), 0, stream,
-                       static_cast<const T*>(x), s, gamma, beta, mean, rstd, a.act, static_cast<T*>(y));
-    return hipGetLastError();
-}
-
-template <int DT>
-hipError_t bwd(const GroupNormArgs& a, const void* x, const void* dy, const float* gamma, const float* beta,
-               const float* mean, const float* rstd, void* dx, float* dgamma, float* dbeta, void* ws,
-               hipStream_t stream) {
-    using T = typename Elt<DT>::T;
-    const Shape s = shape_of(a);
-    float2* sums = static_cast<float2*>(ws);
-    const dim3 grid(unsigned(int64_t(a.n) * a.c));
-    if (a.n > 0) {
-        hipLaunchKernelGGL((k_gn_sums<DT>), grid, dim3(256), 0, stream, static_cast<const T*>(x),
-                           static_cast<const T*>(dy), s, gamma, beta, mean, rstd, a.act, sums);
-        hipLaunchKernelGGL((k_gn_dx<DT>), grid, dim3(256), 0, stream, static_cast<const T*>(x),
-                           static_cast<const T*>(dy), s, gamma, beta, mean, rstd, a.act, sums, static_cast<T*>(dx));
+    part[row][threadIdx.x & 31] = make_float2(a, b);
+    __syncthreads();
+    if (row == 0 && k < c) {
+        a = 0.f, b = 0.f;
+        for (int i = 0; i < 32; ++i) a += part[i][threadIdx.x].x, b += part[i][threadIdx.x].y;
+        if (dgamma) dgamma[k] = b;
+        if (dbeta) dbeta[k] = a;
     }
-    if (dgamma || dbeta)
-        hipLaunchKernelGGL(k_gn_param, dim3(unsigned((a.c + 255) / 256)), dim3(256), 0, stream, sums, a.n, a.c, dgamma,
-                           dbeta);
-    return hipGetLastError();
+}
+
+int log2_ceil(int64_t x) {
+    int l = 0;
+    while ((int64_t(1) << l) < x) ++l;
+    return l;
+}
+int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+int vector_of(int dtype) { return dtype == DT_F16 ? 8 : 4; }
+
+struct Try {
+    int threads, k;
+};
+// Blocks by size, for units of work that there are many of (a few vectors a
+// thread, small blocks) or few of (every thread one or two).
+constexpr Try kMany[] = {{64, 4}, {128, 4}, {256, 4}, {256, 8}, {512, 8}, {1024, 4}, {512, 16}};
+constexpr Try kFew[] = {{64, 2}, {128, 2}, {256, 2}, {512, 2}, {1024, 2}, {1024, 4}, {512, 8}, {512, 16}};
+
+// The lanes that share a row so that a thread has the fewest vectors.
+int64_t rows_slots(int cg, int vpr, int threads, int* lanes_log2, int* vi) {
+    int64_t best = -1;
+    for (int l = 0; (1 << l) <= threads; ++l) {
+        const int64_t v = ceil_div(vpr, 1 << l), n = v * ceil_div(cg, threads >> l);
+        if (best < 0 || n <= best) best = n, *lanes_log2 = l, *vi = int(v);
+    }
+    return best;
+}
+
+// The plan of a call whose tensors allow 16-byte accesses (vec 1: at the
+// beginning of each row, 2: within rows) or not (0).
+Plan plan_rows(const GroupNormArgs& a, bool backward, int vec) {
+    Plan p{};
+    const int v = vec ? vector_of(a.dtype) : 1;
+    Rows& s = p.rows;
+    s.cg = a.c / a.groups, s.groups = a.groups, s.hw = a.h * a.w;
+    s.total = int64_t(a.n) * a.c * s.hw;
+    s.vpr = vec == 2 ? int(ceil_div(s.hw + v - 1, v)) : int(ceil_div(s.hw, v));
+    p.vec = vec;
+    const int64_t units = int64_t(a.n) * a.groups;
+    const auto fits = [&](const Try& t) {
+        if (backward && t.k == 16) return false;
+        const int64_t n = rows_slots(s.cg, s.vpr, t.threads, &s.lanes_log2, &s.vi);
+        if (n > t.k) return false;
+        p.held = true, p.threads = t.threads, p.k = s.slots = int(n), p.grid = units, p.pieces = 1;
+        return true;
+    };
+    if (s.cg <= 4096) {     // the backward's sums of rows fit the LDS
+        if (units >= 512) {
+            for (const Try& t : kMany)
+                if (fits(t)) return p;
+        } else {
+            for (const Try& t : kFew)
+                if (fits(t)) return p;
+        }
+    }
+    p.pieces = int(ceil_div(s.vpr, 64 * (vec ? kPiece : kPieceSingle)));
+    return p;
+}
+
+Plan plan_cols(const GroupNormArgs& a, bool backward, int vec) {
+    Plan p{};
+    const int v = vec ? vector_of(a.dtype) : 1, elt = a.dtype == DT_F16 ? 2 : 4;
+    Cols& s = p.cols;
+    s.c = a.c, s.groups = a.groups, s.cg = a.c / a.groups, s.hw = a.h * a.w;
+    p.vec = vec;
+    int unit = s.cg;        // the fewest channels that are whole groups and whole vectors
+    while (unit % v) unit += s.cg;
+    // Tiles as wide as a cache line, or half or a quarter of one, of whole groups.
+    for (int bytes : {128, 64, 32}) {
+        const int tile = int(ceil_div(bytes, int64_t(unit) * elt)) * unit;
+        s.tile = tile < a.c ? tile : a.c;
+        s.tiles = int(ceil_div(a.c, s.tile));
+        s.cols_log2 = log2_ceil(ceil_div(s.tile, v));
+        if (s.tile > 2048 || s.cols_log2 > 10) continue;        // the LDS, the threads
+        const int64_t units = int64_t(a.n) * s.tiles;
+        if (bytes > 64 && units < 512) continue;
+        const auto fits = [&](const Try& t) {
+            if (t.threads < (1 << s.cols_log2) || (backward && t.k == 16)) return false;
+            const int64_t n = ceil_div(s.hw, t.threads >> s.cols_log2);
+            if (n > t.k) return false;
+            p.held = true, p.threads = t.threads, p.k = int(n), p.pieces = 1;
+            s.pixels = s.hw, s.chunks = 1;
+            p.grid = ceil_div(a.n, 8) * 8 * s.tiles;
+            return true;
+        };
+        if (units >= 512) {
+            for (const Try& t : kMany)
+                if (fits(t)) return p;
+        } else {
+            for (const Try& t : kFew)
+                if (fits(t)) return p;
+        }
+    }
+    // pieces: 256 threads, up to 16 vectors (64 single channels) side by side
+    s.cols_log2 = log2_ceil(ceil_div(a.c, v));
+    const int most = vec ? 4 : 6;
+    if (s.cols_log2 > most) s.cols_log2 = most;
+    s.tile = v << s.cols_log2;
+    s.tiles = int(ceil_div(a.c, s.tile));
+    s.pixels = (256 >> s.cols_log2) * (vec ? kPiece : kPieceSingle);
+    s.chunks = p.pieces = int(ceil_div(s.hw, s.pixels));
+    p.threads = 256;
+    p.grid = ceil_div(a.n, 8) * 8 * s.tiles * s.chunks;
+    return p;
+}
+
+Plan plan_of(const GroupNormArgs& a, bool backward, int vec) {
+    return a.channels_last ? plan_cols(a, backward, vec) : plan_rows(a, backward, vec);
+}
+
+// How the tensors lie: all alike to 16 bytes, and rows (pixels) of whole vectors.
+int vec_of(const GroupNormArgs& a, const void* x, const void* y, const void* z) {
+    const uintptr_t at = reinterpret_cast<uintptr_t>(x) & 15u;
+    for (const void* p : {y, z})
+        if (p && (reinterpret_cast<uintptr_t>(p) & 15u) != at) return 0;
+    const int64_t row = a.channels_last ? a.c : int64_t(a.h) * a.w;
+    if (at == 0 && row % vector_of(a.dtype) == 0) return 1;
+    return a.channels_last ? 0 : 2;
+}
+
+size_t bytes_of(const GroupNormArgs& a, bool backward, int vec) {
+    const Plan p = plan_of(a, backward, vec);
+    const size_t sums = size_t(a.n) * size_t(a.c) * size_t(p.pieces), groups = size_t(a.n) * size_t(a.groups);
+    if (backward) return sums * sizeof(float2) + (p.held ? 0 : groups * sizeof(float2));
+    return p.held ? 0 : sums * sizeof(float4) + groups * 2 * sizeof(float);
 }
 
 }  // namespace
 
+void combine_fwd(const float4* parts, int64_t groups, int per_group, float eps, float* mean, float* rstd, hipStream_t st) {
+    hipLaunchKernelGGL(k_gn_combine_fwd, dim3(unsigned(groups)), dim3(256), 0, st, parts, per_group, eps, mean, rstd);
+}
+void combine_bwd(const float2* parts, int64_t groups, int per_group, int pieces, int groups_per_image, int cg, float m,
+                 const float* gamma, float2* s12, hipStream_t st) {
+    hipLaunchKernelGGL(k_gn_combine_bwd, dim3(unsigned(groups)), dim3(256), 0, st, parts, per_group, pieces,
+                       groups_per_image, cg, m, gamma, s12);
+}
+
+}  // namespace gn
+
+// What the call may need however its tensors lie.
 size_t group_norm_workspace_bytes(const GroupNormArgs& a, bool backward) {
-    const int64_t k = int64_t(a.n) * (backward ? a.c : a.groups);
-    return size_t(k) * 2 * sizeof(float);
+    size_t most = 0;
+    for (int vec : {0, 1, 2}) {
+        const size_t b = gn::bytes_of(a, backward, vec);
+        if (b > most) most = b;
+    }
+    return most;
 }
 
 hipError_t launch_group_norm_fwd(const GroupNormArgs& a, const void* x, const float* gamma, const float* beta, float eps,
                                  void* y, float* mean, float* rstd, void* ws, hipStream_t stream) {
-    return a.dtype == DT_F16 ? fwd<DT_F16>(a, x, gamma, beta, eps, y, mean, rstd, ws, stream)
-                             : fwd<DT_F32>(a, x, gamma, beta, eps, y, mean, rstd, ws, stream);
+    using namespace gn;
+    Plan p = plan_of(a, false, vec_of(a, x, y, nullptr));
+    const Params q{gamma, beta, a.act};
+    float4* parts = static_cast<float4*>(ws);
+    const int64_t rows = int64_t(a.n) * a.c * p.pieces, groups = int64_t(a.n) * a.groups;
+    if (!p.held && !mean) {
+        mean = static_cast<float*>(static_cast<void*>(parts + rows));
+        rstd = mean + groups;
+    }
+    if (a.channels_last) {
+        if (a.dtype == DT_F16) cols_fwd<DT_F16>(p, a.n, x, q, eps, y, mean, rstd, parts, stream);
+        else cols_fwd<DT_F32>(p, a.n, x, q, eps, y, mean, rstd, parts, stream);
+    } else {
+        p.rows.lead = int((reinterpret_cast<uintptr_t>(x) & 15u) / (a.dtype == DT_F16 ? 2 : 4));
+        if (a.dtype == DT_F16) rows_fwd<DT_F16>(p, rows, x, q, eps, y, mean, rstd, parts, stream);
+        else rows_fwd<DT_F32>(p, rows, x, q, eps, y, mean, rstd, parts, stream);
+    }
+    return hipGetLastError();
 }
 
 hipError_t launch_group_norm_bwd(const GroupNormArgs& a, const void* x, const void* dy, const float* gamma,
                                  const float* beta, const float* mean, const float* rstd, void* dx, float* dgamma,
                                  float* dbeta, void* ws, hipStream_t stream) {
-    return a.dtype == DT_F16 ? bwd<DT_F16>(a, x, dy, gamma, beta, mean, rstd, dx, dgamma, dbeta, ws, stream)
-                             : bwd<DT_F32>(a, x, dy, gamma, beta, mean, rstd, dx, dgamma, dbeta, ws, stream);
+    using namespace gn;
+    Plan p = plan_of(a, true, vec_of(a, x, dy, dx));
+    const Params q{gamma, beta, a.act};
+    float2* parts = static_cast<float2*>(ws);
+    const int64_t rows = int64_t(a.n) * a.c * p.pieces;
+    float2* s12 = parts + rows;
+    const bool params = dgamma || dbeta;
+    if (p.held && !params) parts = nullptr;
+    if (a.n > 0) {
+        if (a.channels_last) {
+            if (a.dtype == DT_F16) cols_bwd<DT_F16>(p, a.n, x, dy, q, mean, rstd, dx, parts, s12, stream);
+            else cols_bwd<DT_F32>(p, a.n, x, dy, q, mean, rstd, dx, parts, s12, stream);
+        } else {
+            p.rows.lead = int((reinterpret_cast<uintptr_t>(x) & 15u) / (a.dtype == DT_F16 ? 2 : 4));
+            if (a.dtype == DT_F16) rows_bwd<DT_F16>(p, rows, x, dy, q, mean, rstd, dx, parts, s12, stream);
+            else rows_bwd<DT_F32>(p, rows, x, dy, q, mean, rstd, dx, parts, s12, stream);
+        }
+    }
+    if (params)
+        hipLaunchKernelGGL(k_gn_param, dim3(unsigned((a.c + 31) / 32)), dim3(1024), 0, stream, parts, a.n, a.c, p.pieces,
+                           dgamma, dbeta);
+    return hipGetLastError();
 }
 
 }  // namespace psc
