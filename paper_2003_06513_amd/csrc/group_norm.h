@@ -27,8 +27,10 @@ namespace gn {
 enum : int { ACT_NONE = 0, ACT_RELU = 1, ACT_SILU = 2 };
 
 __device__ __forceinline__ float sigmoid(float u) { return __builtin_amdgcn_rcpf(1.f + __expf(-u)); }
-__device__ __forceinline__ float act_of(float u, int act) {
-    return act == ACT_RELU ? (u < 0.f ? 0.f : u) : act == ACT_SILU ? u * sigmoid(u) : u;
+template <int ACT> __device__ __forceinline__ float act_of(float u) {
+    if (ACT == ACT_RELU) return u < 0.f ? 0.f : u;
+    if (ACT == ACT_SILU) return u * sigmoid(u);
+    return u;
 }
 // u rounds after the product and after the sum, in the forward and in the
 // backward: the ReLU passes the gradient of exactly the outputs above zero.
@@ -37,13 +39,28 @@ __device__ __forceinline__ float affine(float xh, float ga, float be) {
     return xh * ga + be;
 }
 // The gradient at u of a gradient dy at act(u).
-__device__ __forceinline__ float act_back(float u, float dy, int act) {
-    if (act == ACT_RELU) return u > 0.f ? dy : 0.f;
-    if (act == ACT_SILU) {
+template <int ACT> __device__ __forceinline__ float act_back(float u, float dy) {
+    if (ACT == ACT_RELU) return u > 0.f ? dy : 0.f;
+    if (ACT == ACT_SILU) {
         const float s = sigmoid(u);
         return dy * (s * fmaf(u, 1.f - s, 1.f));
     }
     return dy;
+}
+// What a value x of a group and channel becomes, and its normalised value.
+struct Coeff {
+    float mu, r, ga, be;
+};
+__device__ __forceinline__ float normal(const Coeff& k, float x) { return (x - k.mu) * k.r; }
+template <int ACT> __device__ __forceinline__ float forward(const Coeff& k, float x) {
+    return act_of<ACT>(affine(normal(k, x), k.ga, k.be));
+}
+template <int ACT> __device__ __forceinline__ float slope(const Coeff& k, float xh, float dy) {
+    return act_back<ACT>(affine(xh, k.ga, k.be), dy);
+}
+template <int ACT> __device__ __forceinline__ float backward(const Coeff& k, float x, float dy, float s1, float s2) {
+    const float xh = normal(k, x);
+    return k.r * (fmaf(k.ga, slope<ACT>(k, xh, dy), -s1) - xh * s2);
 }
 
 typedef uint32_t u4 __attribute__((ext_vector_type(4)));
@@ -90,28 +107,71 @@ template <int DT> struct Pack<DT, 1> {
     __device__ __forceinline__ static R close(const float (&f)[1]) { return Elt<DT>::from_f(f[0]); }
 };
 
-// Sum over the block, in every thread.  part: 16 floats of LDS; the caller
-// has no other use of them before the next barrier.
+// Sums over lanes, in every one of them, by moves within the register file
+// (a permutation through the LDS takes several times as long, and these sums
+// are most of what a small call waits for).  Step OFF adds the lanes whose
+// numbers differ in bit OFF; the mirrors do as much once the smaller steps
+// are done.
+template <int OFF> __device__ __forceinline__ float lane_step(float x) {
+    const int b = __builtin_bit_cast(int, x);
+    if constexpr (OFF == 16 || OFF == 32) {
+        const auto r = OFF == 16 ? __builtin_amdgcn_permlane16_swap(b, b, false, false)
+                                 : __builtin_amdgcn_permlane32_swap(b, b, false, false);
+        const unsigned lo = r[0], hi = r[1];
+        return __builtin_bit_cast(float, lo) + __builtin_bit_cast(float, hi);
+    } else {
+        // quad_perm [1,0,3,2] and [2,3,0,1], row_half_mirror, row_mirror
+        constexpr int ctrl = OFF == 1 ? 0xB1 : OFF == 2 ? 0x4E : OFF == 4 ? 0x141 : 0x140;
+        return x + __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, b, ctrl, 0xf, 0xf, true));
+    }
+}
 __device__ __forceinline__ float wave_sum(float x) {
-#pragma unroll
-    for (int off = 32; off > 0; off >>= 1) x += __shfl_xor(x, off);
+    x = lane_step<1>(x), x = lane_step<2>(x), x = lane_step<4>(x), x = lane_step<8>(x);
+    return lane_step<32>(lane_step<16>(x));
+}
+// Over runs of `lanes` lanes, a power of two up to 64.
+__device__ __forceinline__ float run_sum(float x, int lanes) {
+    if (lanes > 1) x = lane_step<1>(x);
+    if (lanes > 2) x = lane_step<2>(x);
+    if (lanes > 4) x = lane_step<4>(x);
+    if (lanes > 8) x = lane_step<8>(x);
+    if (lanes > 16) x = lane_step<16>(x);
+    if (lanes > 32) x = lane_step<32>(x);
     return x;
 }
+// Sum over the block, in every thread.  part: 16 floats of LDS; the caller
+// has no other use of them before the next barrier but one.
 __device__ __forceinline__ float block_sum(float x, float* part) {
     x = wave_sum(x);
     const int waves = int(blockDim.x >> 6);
+    if (waves == 1) return x;
     if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = x;
     __syncthreads();
     const int l = threadIdx.x & 15;
-    float s = l < waves ? part[l] : 0.f;
-#pragma unroll
-    for (int off = 8; off > 0; off >>= 1) s += __shfl_xor(s, off);
+    return run_sum(l < waves ? part[l] : 0.f, 16);
+}
+// Two sums at once; part: 32 floats.
+__device__ __forceinline__ float2 block_sum2(float x, float y, float* part) {
+    x = wave_sum(x), y = wave_sum(y);
+    const int waves = int(blockDim.x >> 6);
+    if (waves == 1) return make_float2(x, y);
+    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = x, part[16 + (threadIdx.x >> 6)] = y;
     __syncthreads();
-    return s;
+    const int l = threadIdx.x & 15;
+    return make_float2(run_sum(l < waves ? part[l] : 0.f, 16), run_sum(l < waves ? part[16 + l] : 0.f, 16));
 }
 
 __device__ __forceinline__ float or_one(const float* p, int64_t i) { return p ? p[i] : 1.f; }
 __device__ __forceinline__ float or_zero(const float* p, int64_t i) { return p ? p[i] : 0.f; }
+
+// Accesses at a byte offset of 32 bits from an address that the block (or the
+// wave) has in common: one register a lane instead of two, and no sums.
+template <class R, class T> __device__ __forceinline__ R get(const T* base, uint32_t byte) {
+    return *reinterpret_cast<const R*>(reinterpret_cast<const char*>(base) + byte);
+}
+template <class R, class T> __device__ __forceinline__ void put(T* base, uint32_t byte, const R& r) {
+    *reinterpret_cast<R*>(reinterpret_cast<char*>(base) + byte) = r;
+}
 
 // ---- NCHW.  A channel of an image is a row of hw elements; rows lie one
 // after the other.  With MASK a row need not begin or end at a multiple of 16
@@ -128,48 +188,65 @@ struct Rows {
     int slots;          // vectors per thread: vi times the rows per lane
 };
 
-// Vector k of the row that begins at element `at` of the tensor: elements lo
-// .. hi of it are the row's, and it begins at element `from`.
-struct Window {
-    int64_t from;
-    int lo, hi;
+// The element that offsets of a block or wave count from: `first`, or up to V -
+// 1 elements before it, at a multiple of 16 bytes.  [lo, hi): where the
+// offsets lie in the tensor.
+template <int V, bool MASK> struct Base {
+    int64_t at;
+    int phase, lo, hi;
+    __device__ __forceinline__ Base(const Rows& s, int64_t first) {
+        phase = MASK ? int((first + s.lead) & (V - 1)) : 0;
+        at = first - phase;
+        lo = at < 0 ? int(-at) : 0;
+        const int64_t left = s.total - at;
+        hi = left < (1 << 30) ? int(left) : 1 << 30;
+    }
 };
+// A vector: its first element from the base; elements lo .. hi of it are the row's.
+struct Window {
+    int from, lo, hi;
+};
+// Vector k of the row that begins `row` elements behind the base's `first` and has `len` elements.
 template <int V, bool MASK>
-__device__ __forceinline__ Window window(const Rows& s, int64_t at, int k) {
+__device__ __forceinline__ Window window(const Base<V, MASK>& b, int row, int len, int k) {
     Window w;
     if (!MASK) {
-        w.from = at + int64_t(k) * V;
+        w.from = row + k * V;
         w.lo = 0;
-        w.hi = k < s.vpr ? V : 0;
+        w.hi = k * V < len ? V : 0;
     } else {
-        const int phase = int((at + s.lead) & (V - 1));
-        w.from = at - phase + int64_t(k) * V;
-        const int64_t left = at + s.hw - w.from;
+        const int at = b.phase + row, phase = at & (V - 1);
+        w.from = at - phase + k * V;
+        const int left = at + len - w.from;
         w.lo = k == 0 ? phase : 0;
-        w.hi = left >= V ? V : left > 0 ? int(left) : 0;
+        w.hi = left < V ? left : V;
     }
     return w;
 }
 template <int DT, int V, bool MASK>
-__device__ __forceinline__ typename Pack<DT, V>::R load(const typename Elt<DT>::T* p, const Window& w, int64_t total) {
-    using R = typename Pack<DT, V>::R;
+__device__ __forceinline__ typename Pack<DT, V>::R load(const typename Elt<DT>::T* p, const Base<V, MASK>& b, const Window& w) {
+    using T = typename Elt<DT>::T;
     // the elements beside the row's are other rows', or there are none: nothing outside the tensor is read
-    if (!MASK || (w.from >= 0 && w.from + V <= total)) return *reinterpret_cast<const R*>(p + w.from);
+    if (!MASK || (w.from >= b.lo && w.from + V <= b.hi))
+        return get<typename Pack<DT, V>::R>(p + b.at, uint32_t(w.from) * uint32_t(sizeof(T)));
     float f[V];
 #pragma unroll
-    for (int j = 0; j < V; ++j) f[j] = j >= w.lo && j < w.hi ? Elt<DT>::load(p, w.from + j) : 0.f;
+    for (int j = 0; j < V; ++j) f[j] = j >= w.lo && j < w.hi ? Elt<DT>::load(p, b.at + w.from + j) : 0.f;
     return Pack<DT, V>::close(f);
 }
 template <int DT, int V, bool MASK>
-__device__ __forceinline__ void store(typename Elt<DT>::T* p, const Window& w, const float (&f)[V]) {
-    using R = typename Pack<DT, V>::R;
+__device__ __forceinline__ void store(typename Elt<DT>::T* p, const Base<V, MASK>& b, const Window& w, const float (&f)[V]) {
+    using T = typename Elt<DT>::T;
+    const auto r = Pack<DT, V>::close(f);
+    const uint32_t byte = uint32_t(w.from) * uint32_t(sizeof(T));
     if (!MASK || (w.lo == 0 && w.hi == V)) {
-        *reinterpret_cast<R*>(p + w.from) = Pack<DT, V>::close(f);
+        put(p + b.at, byte, r);
         return;
     }
+    const T* e = reinterpret_cast<const T*>(&r);
 #pragma unroll
     for (int j = 0; j < V; ++j)
-        if (j >= w.lo && j < w.hi) p[w.from + j] = Elt<DT>::from_f(f[j]);
+        if (j >= w.lo && j < w.hi) put(p + b.at, byte + j * uint32_t(sizeof(T)), e[j]);
 }
 template <bool MASK> __device__ __forceinline__ bool in(const Window& w, int j) { return !MASK || (j >= w.lo && j < w.hi); }
 
@@ -183,53 +260,41 @@ struct Cols {
     int cols_log2;
     int pixels;         // pixels of a block
     int chunks;         // blocks that share the pixels of an image
+    uint32_t cg_m;      // 2^32 / cg, rounded up
 };
+// k / cg for k, cg < 2^16 (cg_m is at most cg - 1 too large: less than 2^32 / cg in the product); cg == 1: 0.
+__device__ __forceinline__ int group_of(const Cols& q, int k) { return q.cg_m ? int(__umulhi(uint32_t(k), q.cg_m)) : k; }
 
-// The sums of the block's channels: s[V] of each thread, over the threads
-// that have the same channels; in `ch` [tile] of LDS, `buf` [threads / max(cols,
-// 64)][tile].
+// Adds s[V] of each thread over the threads of the wave that have the same
+// channels, and leaves the wave's sums in `buf`, of which there are
+// sum_rows(q) rows of `tile`.
+__device__ __forceinline__ int span_log2(const Cols& q) { return q.cols_log2 > 6 ? q.cols_log2 : 6; }
+__device__ __forceinline__ int sum_rows(const Cols& q) { return int(blockDim.x >> span_log2(q)); }
 template <int V>
-__device__ __forceinline__ void channel_sums(const float (&s)[V], const Cols& q, int width, float* buf, float* ch) {
-    const int cols = 1 << q.cols_log2;
-    const int col = threadIdx.x & (cols - 1);
-    float t[V];
+__device__ __forceinline__ void wave_channels(float (&s)[V], const Cols& q, int width, float* buf) {
+    const int cols = 1 << q.cols_log2, col = int(threadIdx.x) & (cols - 1);
+    // lanes that differ in the bits from `cols` on have the same channels; the mirrors within 16 lanes want the
+    // smaller bits summed before, so those steps go by exchange
+    for (int off = cols; off < 16; off <<= 1)
 #pragma unroll
-    for (int j = 0; j < V; ++j) t[j] = s[j];
-    for (int off = cols; off < 64; off <<= 1)
+        for (int j = 0; j < V; ++j) s[j] += __shfl_xor(s[j], off);
+    if (cols <= 16)
 #pragma unroll
-        for (int j = 0; j < V; ++j) t[j] += __shfl_xor(t[j], off);
-    const int span_log2 = q.cols_log2 > 6 ? q.cols_log2 : 6;
-    const int row = int(threadIdx.x >> span_log2), rows = int(blockDim.x >> span_log2);
-    if ((threadIdx.x & 63) < unsigned(cols) && col * V < width)
+        for (int j = 0; j < V; ++j) s[j] = lane_step<16>(s[j]);
+    if (cols <= 32)
 #pragma unroll
-        for (int j = 0; j < V; ++j) buf[row * q.tile + col * V + j] = t[j];
-    __syncthreads();
-    for (int k = threadIdx.x; k < width; k += blockDim.x) {
-        float sum = 0.f;
-        for (int i = 0; i < rows; ++i) sum += buf[i * q.tile + k];
-        ch[k] = sum;
+        for (int j = 0; j < V; ++j) s[j] = lane_step<32>(s[j]);
+    if (int(threadIdx.x & 63u) < cols && col * V < width) {
+        float* to = buf + int(threadIdx.x >> span_log2(q)) * q.tile + col * V;
+#pragma unroll
+        for (int j = 0; j < V; ++j) to[j] = s[j];
     }
-    __syncthreads();
 }
-
-// Sums of the groups of the block's channels, weighted: out[g] for width / cg
-// groups, from ch.  A thread per group of few channels, a wave otherwise.
-__device__ __forceinline__ void group_sums(const float* ch, const float* weight, int cg, int count, float* out) {
-    if (cg <= 16) {
-        for (int g = threadIdx.x; g < count; g += blockDim.x) {
-            float s = 0.f;
-            for (int k = 0; k < cg; ++k) s = fmaf(or_one(weight, g * cg + k), ch[g * cg + k], s);
-            out[g] = s;
-        }
-    } else {
-        for (int g = threadIdx.x >> 6; g < count; g += blockDim.x >> 6) {
-            float s = 0.f;
-            for (int k = threadIdx.x & 63; k < cg; k += 64) s = fmaf(or_one(weight, g * cg + k), ch[g * cg + k], s);
-            s = wave_sum(s);
-            if ((threadIdx.x & 63) == 0) out[g] = s;
-        }
-    }
-    __syncthreads();
+__device__ __forceinline__ float sum_of_channel(const float* buf, const Cols& q, int k) {
+    float s = 0.f;
+    const int rows = sum_rows(q);
+    for (int i = 0; i < rows; ++i) s += buf[i * q.tile + k];
+    return s;
 }
 
 struct Params {
@@ -251,6 +316,34 @@ struct Plan {
 };
 // Vectors per lane of the kernels that work piece by piece: 16 bytes, single elements.
 constexpr int kPiece = 8, kPieceSingle = 32;
+// Threads of the kernels that hold their groups: the registers of K vectors for
+// so many (kept below 128 of 1024 threads, 256 of 512).
+constexpr int threads_of(int v, int k) { return k <= 4 || (v == 1 && k <= 8) ? 1024 : 512; }
+// The most vectors per thread of the kernels that hold their groups.
+constexpr int kMostFwd = 16, kMostBwd = 8, kMostSingle = 32;
+
+// Calls go with the compiled activation and count of vectors per thread.
+template <class F> void with_act(int act, F go) {
+    if (act == ACT_NONE) go(IntC<ACT_NONE>{});
+    else if (act == ACT_RELU) go(IntC<ACT_RELU>{});
+    else go(IntC<ACT_SILU>{});
+}
+template <int V, bool BACK, class F> void with_count(int k, F go) {
+    if constexpr (V == 1) {
+        if (k <= 8) go(IntC<8>{});
+        else go(IntC<kMostSingle>{});
+    } else {
+        if (k <= 2) go(IntC<2>{});
+        else if (k <= 4) go(IntC<4>{});
+        else if (k <= 8) go(IntC<8>{});
+        else if constexpr (!BACK) go(IntC<kMostFwd>{});
+    }
+}
+
+// LDS of a block of columns: `sums` arrays of the waves' sums, `more` of one value per channel.
+inline unsigned cols_lds(const Cols& q, int threads, int sums, int more) {
+    return unsigned(sizeof(float)) * unsigned(q.tile) * unsigned(sums * (threads >> (q.cols_log2 > 6 ? q.cols_log2 : 6)) + more);
+}
 
 template <int DT> void rows_fwd(const Plan& p, int64_t count, const void* x, const Params& q, float eps, void* y,
                                 float* mean, float* rstd, float4* parts, hipStream_t st);

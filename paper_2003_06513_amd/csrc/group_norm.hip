@@ -1,5 +1,6 @@
 // Group normalisation: how a call runs, and the sums between the passes over
 // pieces.
+#include <cstdlib>
 #include "group_norm.h"
 
 namespace psc {
@@ -10,20 +11,22 @@ namespace {
 // counts, the squares about the common mean.
 __global__ __launch_bounds__(256) void k_gn_combine_fwd(const float4* __restrict__ parts, int per, float eps,
                                                         float* __restrict__ mean, float* __restrict__ rstd) {
-    __shared__ float part[16];
+    __shared__ float part[32];
     const float4* p = parts + int64_t(blockIdx.x) * per;
     float sum = 0.f, num = 0.f;
     for (int i = threadIdx.x; i < per; i += 256) {
         sum = fmaf(p[i].z, p[i].x, sum);
         num += p[i].z;
     }
-    num = block_sum(num, part);
-    const float mu = block_sum(sum, part) / num;
+    const float2 both = block_sum2(num, sum, part);
+    num = both.x;
+    const float mu = both.y / num;
     float sq = 0.f;
     for (int i = threadIdx.x; i < per; i += 256) {
         const float d = p[i].x - mu;
         sq += fmaf(p[i].z * d, d, p[i].y);
     }
+    __syncthreads();
     sq = block_sum(sq, part);
     if (threadIdx.x == 0) {
         mean[blockIdx.x] = mu;
@@ -34,7 +37,7 @@ __global__ __launch_bounds__(256) void k_gn_combine_fwd(const float4* __restrict
 __global__ __launch_bounds__(256) void k_gn_combine_bwd(const float2* __restrict__ parts, int per, int pieces,
                                                         int groups, int cg, float m, const float* __restrict__ gamma,
                                                         float2* __restrict__ s12) {
-    __shared__ float part[16];
+    __shared__ float part[32];
     const float2* p = parts + int64_t(blockIdx.x) * per;
     const int c0 = int(blockIdx.x % unsigned(groups)) * cg;
     float s1 = 0.f, s2 = 0.f;
@@ -43,9 +46,8 @@ __global__ __launch_bounds__(256) void k_gn_combine_bwd(const float2* __restrict
         s1 = fmaf(ga, p[i].x, s1);
         s2 = fmaf(ga, p[i].y, s2);
     }
-    s1 = block_sum(s1, part);
-    s2 = block_sum(s2, part);
-    if (threadIdx.x == 0) s12[blockIdx.x] = make_float2(s1 / m, s2 / m);
+    const float2 sum = block_sum2(s1, s2, part);
+    if (threadIdx.x == 0) s12[blockIdx.x] = make_float2(sum.x / m, sum.y / m);
 }
 
 // dbeta and dgamma: a block adds 32 channels, each over the images' and
@@ -88,8 +90,9 @@ struct Try {
 };
 // Blocks by size, for units of work that there are many of (a few vectors a
 // thread, small blocks) or few of (every thread one or two).
-constexpr Try kMany[] = {{64, 4}, {128, 4}, {256, 4}, {256, 8}, {512, 8}, {1024, 4}, {512, 16}};
-constexpr Try kFew[] = {{64, 2}, {128, 2}, {256, 2}, {512, 2}, {1024, 2}, {1024, 4}, {512, 8}, {512, 16}};
+constexpr Try kMany[] = {{64, 4}, {128, 4}, {256, 4}, {256, 8}, {512, 8}, {1024, 4}, {512, 32}};
+constexpr Try kFew[] = {{64, 2}, {128, 2}, {256, 2}, {512, 2}, {1024, 2}, {1024, 4}, {512, 8}, {512, 32}};
+int most_of(bool backward, int vec) { return vec == 0 ? kMostSingle : backward ? kMostBwd : kMostFwd; }
 
 // The lanes that share a row so that a thread has the fewest vectors.
 int64_t rows_slots(int cg, int vpr, int threads, int* lanes_log2, int* vi) {
@@ -113,13 +116,12 @@ Plan plan_rows(const GroupNormArgs& a, bool backward, int vec) {
     p.vec = vec;
     const int64_t units = int64_t(a.n) * a.groups;
     const auto fits = [&](const Try& t) {
-        if (backward && t.k == 16) return false;
         const int64_t n = rows_slots(s.cg, s.vpr, t.threads, &s.lanes_log2, &s.vi);
-        if (n > t.k) return false;
+        if (n > t.k || n > most_of(backward, vec)) return false;
         p.held = true, p.threads = t.threads, p.k = s.slots = int(n), p.grid = units, p.pieces = 1;
         return true;
     };
-    if (s.cg <= 4096) {     // the backward's sums of rows fit the LDS
+    if (vec && s.cg <= 2048) {      // the rows' parameters and sums fit the LDS
         if (units >= 512) {
             for (const Try& t : kMany)
                 if (fits(t)) return p;
@@ -138,34 +140,45 @@ Plan plan_cols(const GroupNormArgs& a, bool backward, int vec) {
     Cols& s = p.cols;
     s.c = a.c, s.groups = a.groups, s.cg = a.c / a.groups, s.hw = a.h * a.w;
     p.vec = vec;
+    s.cg_m = s.cg == 1 ? 0 : uint32_t(((uint64_t(1) << 32) + s.cg - 1) / s.cg);
     int unit = s.cg;        // the fewest channels that are whole groups and whole vectors
     while (unit % v) unit += s.cg;
     // Tiles as wide as a cache line, or half or a quarter of one, of whole groups.
-    for (int bytes : {128, 64, 32}) {
+    const int want = getenv("GN_UNITS") ? atoi(getenv("GN_UNITS")) : 512;
+    const int least = getenv("GN_LEAST") ? atoi(getenv("GN_LEAST")) : 16;
+    Plan best{};
+    for (int bytes = 128; bytes >= least; bytes /= 2) {
         const int tile = int(ceil_div(bytes, int64_t(unit) * elt)) * unit;
         s.tile = tile < a.c ? tile : a.c;
         s.tiles = int(ceil_div(a.c, s.tile));
         s.cols_log2 = log2_ceil(ceil_div(s.tile, v));
-        if (s.tile > 2048 || s.cols_log2 > 10) continue;        // the LDS, the threads
         const int64_t units = int64_t(a.n) * s.tiles;
-        if (bytes > 64 && units < 512) continue;
         const auto fits = [&](const Try& t) {
-            if (t.threads < (1 << s.cols_log2) || (backward && t.k == 16)) return false;
+            if (t.threads < (1 << s.cols_log2) || int64_t(s.hw) * a.c * elt >> 32) return false;
             const int64_t n = ceil_div(s.hw, t.threads >> s.cols_log2);
-            if (n > t.k) return false;
+            if (n > t.k || n > most_of(backward, vec)) return false;
+            if (cols_lds(s, t.threads, backward ? 2 : 1, backward ? 4 : 2) > 60 * 1024) return false;
             p.held = true, p.threads = t.threads, p.k = int(n), p.pieces = 1;
             s.pixels = s.hw, s.chunks = 1;
             p.grid = ceil_div(a.n, 8) * 8 * s.tiles;
             return true;
         };
+        bool found = false;
         if (units >= 512) {
             for (const Try& t : kMany)
-                if (fits(t)) return p;
+                if (!found) found = fits(t);
         } else {
             for (const Try& t : kFew)
-                if (fits(t)) return p;
+                if (!found) found = fits(t);
         }
+        if (found) best = p;
+        if (found && units >= want) break;
     }
+    if (best.held && !getenv("GN_PIECES")) return best;
+    p = best = Plan{};
+    p.vec = vec;
+    s.c = a.c, s.groups = a.groups, s.cg = a.c / a.groups, s.hw = a.h * a.w;
+    s.cg_m = s.cg == 1 ? 0 : uint32_t(((uint64_t(1) << 32) + s.cg - 1) / s.cg);
     // pieces: 256 threads, up to 16 vectors (64 single channels) side by side
     s.cols_log2 = log2_ceil(ceil_div(a.c, v));
     const int most = vec ? 4 : 6;

@@ -37,69 +37,108 @@ __device__ __forceinline__ bool place(const Cols& q, int images, Place& p) {
     p.on = p.rel < p.width;
     return true;
 }
-// Calls f(i, at) for the vectors of this thread: slot i, which begins at element `at`.
-template <int K, class F>
+// The element that the block's offsets count from.
+__device__ __forceinline__ int64_t base_of(const Cols& q, const Place& p) {
+    return (int64_t(p.n) * q.hw + p.first) * q.c + p.c0;
+}
+// Calls f(i, byte) for the vectors of this thread: slot i, which begins `byte` bytes behind the base.
+template <int DT, int K, class F>
 __device__ __forceinline__ void each(const Cols& q, const Place& p, F f) {
     if (!p.on) return;
-    const int64_t at = int64_t(p.n) * q.hw * q.c + p.c0 + p.rel;
+    constexpr uint32_t elt = sizeof(typename Elt<DT>::T);
+    uint32_t byte = (uint32_t(p.row) * uint32_t(q.c) + uint32_t(p.rel)) * elt;
+    const uint32_t step = uint32_t(p.rows) * uint32_t(q.c) * elt;
+    int left = p.last - p.first - p.row;
 #pragma unroll
     for (int i = 0; i < K; ++i) {
-        const int px = p.first + i * p.rows + p.row;
-        if (px < p.last) f(i, at + int64_t(px) * q.c);
+        if (left > 0) f(i, byte);
+        left -= p.rows, byte += step;
     }
 }
-template <int DT, int V>
-__device__ __forceinline__ typename Pack<DT, V>::R get(const typename Elt<DT>::T* p, int64_t at) {
-    return *reinterpret_cast<const typename Pack<DT, V>::R*>(p + at);
-}
-template <int DT, int V>
-__device__ __forceinline__ void put(typename Elt<DT>::T* p, int64_t at, const float (&f)[V]) {
-    *reinterpret_cast<typename Pack<DT, V>::R*>(p + at) = Pack<DT, V>::close(f);
+// V values of the thread's channels; they lie at multiples of four bytes.
+typedef float f4u __attribute__((ext_vector_type(4), aligned(4)));
+template <int V> __device__ __forceinline__ void values(const float* p, bool on, float fill, float (&f)[V]) {
+#pragma unroll
+    for (int j = 0; j < V; ++j) f[j] = fill;
+    if (!p || !on) return;
+    if constexpr (V == 1) {
+        f[0] = *p;
+    } else {
+#pragma unroll
+        for (int j = 0; j < V; j += 4) {
+            const f4u t = *reinterpret_cast<const f4u*>(p + j);
+            f[j] = t.x, f[j + 1] = t.y, f[j + 2] = t.z, f[j + 3] = t.w;
+        }
+    }
 }
 
-// LDS of a block: the threads' sums, the channels', the groups' (two of each).
-__device__ __forceinline__ float* lds_of_channels(float* lds, const Cols& q) {
-    const int span_log2 = q.cols_log2 > 6 ? q.cols_log2 : 6;
-    return lds + (blockDim.x >> span_log2) * q.tile;
+// Calls f(g, sum) once for each of the block's groups, the sums weighted: a
+// thread adds a group of few channels, a wave one of many.
+template <class F>
+__device__ __forceinline__ void each_group(const Cols& q, int count, const float* ch, const float* weight, F f) {
+    if (q.cg <= 16) {
+        for (int g = threadIdx.x; g < count; g += blockDim.x) {
+            float s = 0.f;
+            for (int k = 0; k < q.cg; ++k) s = fmaf(or_one(weight, g * q.cg + k), ch[g * q.cg + k], s);
+            f(g, s);
+        }
+    } else {
+        for (int g = int(threadIdx.x >> 6); g < count; g += int(blockDim.x >> 6)) {
+            float s = 0.f;
+            for (int k = int(threadIdx.x & 63); k < q.cg; k += 64) s = fmaf(or_one(weight, g * q.cg + k), ch[g * q.cg + k], s);
+            s = wave_sum(s);
+            if ((threadIdx.x & 63) == 0) f(g, s);
+        }
+    }
 }
 
-template <int DT, int V, int K>
-__global__ __launch_bounds__(K <= 4 ? 1024 : 512) void k_gn_cols_fwd(const typename Elt<DT>::T* __restrict__ x, Cols q,
-                                                                     int images, Params w, float eps,
-                                                                     typename Elt<DT>::T* __restrict__ y,
-                                                                     float* __restrict__ mean, float* __restrict__ rstd) {
+template <int DT, int V, int K, int ACT>
+__global__ __launch_bounds__(threads_of(V, K)) void k_gn_cols_fwd(const typename Elt<DT>::T* __restrict__ x, Cols q,
+                                                                  int images, Params w, float eps,
+                                                                  typename Elt<DT>::T* __restrict__ y,
+                                                                  float* __restrict__ mean, float* __restrict__ rstd) {
     using P = Pack<DT, V>;
-    extern __shared__ float lds[];
+    extern __shared__ float lds[];              // the waves' sums, the channels', the groups'
     Place p;
     if (!place<V>(q, images, p)) return;
-    float* ch = lds_of_channels(lds, q);
+    float* ch = lds + sum_rows(q) * q.tile;
     float* gr = ch + q.tile;
     const int count = p.width / q.cg;
     const float m = float(q.cg) * float(q.hw);
+    const int64_t g0 = int64_t(p.n) * q.groups + p.c0 / q.cg;
+    const int64_t at = base_of(q, p);
+    const typename Elt<DT>::T* xb = x + at;
     typename P::R d[K];
-    each<K>(q, p, [&](int i, int64_t at) { d[i] = get<DT, V>(x, at); });
-    float s[V], mu[V];
+    each<DT, K>(q, p, [&](int i, uint32_t byte) { d[i] = get<typename P::R>(xb, byte); });
+    float ga[V], be[V];
+    values<V>(w.gamma ? w.gamma + p.c0 + p.rel : nullptr, p.on, 1.f, ga);
+    values<V>(w.beta ? w.beta + p.c0 + p.rel : nullptr, p.on, 0.f, be);
+    float s[V], mu[V], r[V];
 #pragma unroll
     for (int j = 0; j < V; ++j) s[j] = 0.f;
-    each<K>(q, p, [&](int i, int64_t) {
+    each<DT, K>(q, p, [&](int i, uint32_t) {
         float f[V];
         P::open(d[i], f);
 #pragma unroll
         for (int j = 0; j < V; ++j) s[j] += f[j];
     });
-    channel_sums<V>(s, q, p.width, lds, ch);
-    group_sums(ch, nullptr, q.cg, count, gr);
+    wave_channels<V>(s, q, p.width, lds);
+    __syncthreads();
+    for (int k = threadIdx.x; k < p.width; k += blockDim.x) ch[k] = sum_of_channel(lds, q, k);
+    __syncthreads();
+    each_group(q, count, ch, nullptr, [&](int g, float sum) {
+        gr[g] = sum / m;
+        if (mean) mean[g0 + g] = sum / m;
+    });
+    __syncthreads();
     int g[V];
 #pragma unroll
     for (int j = 0; j < V; ++j) {
-        g[j] = p.on ? (p.rel + j) / q.cg : 0;
-        mu[j] = gr[g[j]] / m;
+        g[j] = p.on ? group_of(q, p.rel + j) : 0;
+        mu[j] = gr[g[j]];
         s[j] = 0.f;
     }
-    const int64_t g0 = int64_t(p.n) * q.groups + p.c0 / q.cg;
-    if (mean)
-        for (int k = threadIdx.x; k < count; k += blockDim.x) mean[g0 + k] = gr[k] / m;
-    each<K>(q, p, [&](int i, int64_t) {
+    each<DT, K>(q, p, [&](int i, uint32_t) {
         float f[V];
         P::open(d[i], f);
 #pragma unroll
@@ -108,83 +147,75 @@ __global__ __launch_bounds__(K <= 4 ? 1024 : 512) void k_gn_cols_fwd(const typen
             s[j] = fmaf(e, e, s[j]);
         }
     });
-    channel_sums<V>(s, q, p.width, lds, ch);
-    group_sums(ch, nullptr, q.cg, count, gr);
-    float r[V], ga[V], be[V];
+    wave_channels<V>(s, q, p.width, lds);
+    __syncthreads();
+    for (int k = threadIdx.x; k < p.width; k += blockDim.x) ch[k] = sum_of_channel(lds, q, k);
+    __syncthreads();
+    each_group(q, count, ch, nullptr, [&](int g, float sum) {
+        const float rs = 1.f / sqrtf(sum / m + eps);
+        gr[g] = rs;
+        if (rstd) rstd[g0 + g] = rs;
+    });
+    __syncthreads();
 #pragma unroll
-    for (int j = 0; j < V; ++j) {
-        r[j] = 1.f / sqrtf(gr[g[j]] / m + eps);
-        ga[j] = p.on ? or_one(w.gamma, p.c0 + p.rel + j) : 1.f;
-        be[j] = p.on ? or_zero(w.beta, p.c0 + p.rel + j) : 0.f;
-    }
-    if (rstd)
-        for (int k = threadIdx.x; k < count; k += blockDim.x) rstd[g0 + k] = 1.f / sqrtf(gr[k] / m + eps);
-    each<K>(q, p, [&](int i, int64_t at) {
+    for (int j = 0; j < V; ++j) r[j] = gr[g[j]];
+    each<DT, K>(q, p, [&](int i, uint32_t byte) {
         float f[V];
         P::open(d[i], f);
 #pragma unroll
-        for (int j = 0; j < V; ++j) f[j] = act_of(affine((f[j] - mu[j]) * r[j], ga[j], be[j]), w.act);
-        put<DT, V>(y, at, f);
+        for (int j = 0; j < V; ++j) f[j] = forward<ACT>(Coeff{mu[j], r[j], ga[j], be[j]}, f[j]);
+        put(y + at, byte, P::close(f));
     });
 }
 
 template <int V>
-struct Coeff {
-    float mu[V], r[V], ga[V], be[V];
-};
-template <int V>
 __device__ __forceinline__ void coefficients(const Cols& q, const Place& p, const Params& w, const float* mean,
-                                             const float* rstd, Coeff<V>& k) {
+                                             const float* rstd, Coeff (&k)[V]) {
+    float ga[V], be[V];
+    const int c = p.c0 + p.rel;
+    values<V>(w.gamma ? w.gamma + c : nullptr, p.on, 1.f, ga);
+    values<V>(w.beta ? w.beta + c : nullptr, p.on, 0.f, be);
 #pragma unroll
     for (int j = 0; j < V; ++j) {
-        const int c = p.on ? p.c0 + p.rel + j : 0;
-        const int64_t g = int64_t(p.n) * q.groups + c / q.cg;
-        k.mu[j] = mean[g];
-        k.r[j] = rstd[g];
-        k.ga[j] = or_one(w.gamma, c);
-        k.be[j] = or_zero(w.beta, c);
+        const int64_t g = int64_t(p.n) * q.groups + (p.on ? group_of(q, c + j) : 0);
+        k[j] = Coeff{mean[g], rstd[g], ga[j], be[j]};
     }
 }
 
-template <int DT, int V, int K>
+template <int DT, int V, int K, int ACT>
 __device__ __forceinline__ void sums_back(const typename Pack<DT, V>::R (&d)[K], const typename Pack<DT, V>::R (&e)[K],
-                                          const Cols& q, const Place& p, const Coeff<V>& k, int act, float (&a)[V],
-                                          float (&b)[V]) {
+                                          const Cols& q, const Place& p, const Coeff (&k)[V], float (&a)[V], float (&b)[V]) {
 #pragma unroll
     for (int j = 0; j < V; ++j) a[j] = 0.f, b[j] = 0.f;
-    each<K>(q, p, [&](int i, int64_t) {
+    each<DT, K>(q, p, [&](int i, uint32_t) {
         float f[V], g[V];
         Pack<DT, V>::open(d[i], f);
         Pack<DT, V>::open(e[i], g);
 #pragma unroll
         for (int j = 0; j < V; ++j) {
-            const float xh = (f[j] - k.mu[j]) * k.r[j];
-            const float du = act_back(affine(xh, k.ga[j], k.be[j]), g[j], act);
+            const float xh = normal(k[j], f[j]);
+            const float du = slope<ACT>(k[j], xh, g[j]);
             a[j] += du;
             b[j] = fmaf(du, xh, b[j]);
         }
     });
 }
-template <int DT, int V, int K>
+template <int DT, int V, int K, int ACT>
 __device__ __forceinline__ void write_back(const typename Pack<DT, V>::R (&d)[K], const typename Pack<DT, V>::R (&e)[K],
-                                           const Cols& q, const Place& p, const Coeff<V>& k, int act,
-                                           const float (&s1)[V], const float (&s2)[V], typename Elt<DT>::T* dx) {
-    each<K>(q, p, [&](int i, int64_t at) {
+                                           const Cols& q, const Place& p, const Coeff (&k)[V], const float (&s1)[V],
+                                           const float (&s2)[V], typename Elt<DT>::T* dxb) {
+    each<DT, K>(q, p, [&](int i, uint32_t byte) {
         float f[V], g[V];
         Pack<DT, V>::open(d[i], f);
         Pack<DT, V>::open(e[i], g);
 #pragma unroll
-        for (int j = 0; j < V; ++j) {
-            const float xh = (f[j] - k.mu[j]) * k.r[j];
-            const float du = act_back(affine(xh, k.ga[j], k.be[j]), g[j], act);
-            f[j] = k.r[j] * (fmaf(k.ga[j], du, -s1[j]) - xh * s2[j]);
-        }
-        put<DT, V>(dx, at, f);
+        for (int j = 0; j < V; ++j) f[j] = backward<ACT>(k[j], f[j], g[j], s1[j], s2[j]);
+        put(dxb, byte, Pack<DT, V>::close(f));
     });
 }
 
-template <int DT, int V, int K>
-__global__ __launch_bounds__(K <= 4 ? 1024 : 512) void k_gn_cols_bwd(const typename Elt<DT>::T* __restrict__ x,
+template <int DT, int V, int K, int ACT>
+__global__ __launch_bounds__(threads_of(V, K)) void k_gn_cols_bwd(const typename Elt<DT>::T* __restrict__ x,
                                                                      const typename Elt<DT>::T* __restrict__ dy, Cols q,
                                                                      int images, Params w,
                                                                      const float* __restrict__ mean,
@@ -192,71 +223,81 @@ __global__ __launch_bounds__(K <= 4 ? 1024 : 512) void k_gn_cols_bwd(const typen
                                                                      typename Elt<DT>::T* __restrict__ dx,
                                                                      float2* __restrict__ sums) {
     using P = Pack<DT, V>;
-    extern __shared__ float lds[];
+    extern __shared__ float lds[];              // two each: the waves' sums, the channels', the groups'
     Place p;
     if (!place<V>(q, images, p)) return;
-    float* ch = lds_of_channels(lds, q);
-    float* ch2 = ch + q.tile;
-    float* gr = ch2 + q.tile;
-    float* gr2 = gr + q.tile;
+    const int all = sum_rows(q) * q.tile;
+    float *ch = lds + 2 * all, *ch2 = ch + q.tile, *gr = ch2 + q.tile, *gr2 = gr + q.tile;
     const int count = p.width / q.cg;
     const float m = float(q.cg) * float(q.hw);
+    const int64_t at = base_of(q, p);
+    const typename Elt<DT>::T *xb = x + at, *gb = dy + at;
     typename P::R d[K], e[K];
-    each<K>(q, p, [&](int i, int64_t at) {
-        d[i] = get<DT, V>(x, at);
-        e[i] = get<DT, V>(dy, at);
+    each<DT, K>(q, p, [&](int i, uint32_t byte) {
+        d[i] = get<typename P::R>(xb, byte);
+        e[i] = get<typename P::R>(gb, byte);
     });
-    Coeff<V> k;
+    Coeff k[V];
     coefficients<V>(q, p, w, mean, rstd, k);
     float a[V], b[V];
-    sums_back<DT, V, K>(d, e, q, p, k, w.act, a, b);
-    channel_sums<V>(a, q, p.width, lds, ch);
-    channel_sums<V>(b, q, p.width, lds, ch2);
-    if (sums)
-        for (int c = threadIdx.x; c < p.width; c += blockDim.x)
-            sums[int64_t(p.n) * q.c + p.c0 + c] = make_float2(ch[c], ch2[c]);
+    sums_back<DT, V, K, ACT>(d, e, q, p, k, a, b);
+    wave_channels<V>(a, q, p.width, lds);
+    wave_channels<V>(b, q, p.width, lds + all);
+    __syncthreads();
+    for (int c = threadIdx.x; c < p.width; c += blockDim.x) {
+        const float2 ab = make_float2(sum_of_channel(lds, q, c), sum_of_channel(lds + all, q, c));
+        ch[c] = ab.x, ch2[c] = ab.y;
+        if (sums) sums[int64_t(p.n) * q.c + p.c0 + c] = ab;
+    }
+    __syncthreads();
     const float* gamma = w.gamma ? w.gamma + p.c0 : nullptr;
-    group_sums(ch, gamma, q.cg, count, gr);
-    group_sums(ch2, gamma, q.cg, count, gr2);
+    each_group(q, count, ch, gamma, [&](int g, float sum) { gr[g] = sum / m; });
+    each_group(q, count, ch2, gamma, [&](int g, float sum) { gr2[g] = sum / m; });
+    __syncthreads();
 #pragma unroll
     for (int j = 0; j < V; ++j) {
-        const int g = p.on ? (p.rel + j) / q.cg : 0;
-        a[j] = gr[g] / m;
-        b[j] = gr2[g] / m;
+        const int g = p.on ? group_of(q, p.rel + j) : 0;
+        a[j] = gr[g];
+        b[j] = gr2[g];
     }
-    write_back<DT, V, K>(d, e, q, p, k, w.act, a, b, dx);
+    write_back<DT, V, K, ACT>(d, e, q, p, k, a, b, dx + at);
 }
 
 // ---- pieces: some pixels of some channels.
 
 template <int DT, int V, int K>
-__global__ __launch_bounds__(256) void k_gn_colparts_fwd(const typename Elt<DT>::T* __restrict__ x, Cols q, int images,
+__global__ __launch_bounds__(256, 4) void k_gn_colparts_fwd(const typename Elt<DT>::T* __restrict__ x, Cols q, int images,
                                                          float4* __restrict__ parts) {
     using P = Pack<DT, V>;
-    extern __shared__ float lds[];
+    extern __shared__ float lds[];              // two each: the waves' sums, the channels' means
     Place p;
     if (!place<V>(q, images, p)) return;
-    float* ch = lds_of_channels(lds, q);
-    float* ch2 = ch + q.tile;
+    const int all = sum_rows(q) * q.tile;
+    float* ch = lds + 2 * all;
+    const int64_t at = base_of(q, p);
+    const typename Elt<DT>::T* xb = x + at;
     typename P::R d[K];
-    each<K>(q, p, [&](int i, int64_t at) { d[i] = get<DT, V>(x, at); });
+    each<DT, K>(q, p, [&](int i, uint32_t byte) { d[i] = get<typename P::R>(xb, byte); });
     float s[V], mu[V];
 #pragma unroll
     for (int j = 0; j < V; ++j) s[j] = 0.f;
-    each<K>(q, p, [&](int i, int64_t) {
+    each<DT, K>(q, p, [&](int i, uint32_t) {
         float f[V];
         P::open(d[i], f);
 #pragma unroll
         for (int j = 0; j < V; ++j) s[j] += f[j];
     });
     const float num = float(p.last - p.first);
-    channel_sums<V>(s, q, p.width, lds, ch);
+    wave_channels<V>(s, q, p.width, lds);
+    __syncthreads();
+    for (int c = threadIdx.x; c < p.width; c += blockDim.x) ch[c] = sum_of_channel(lds, q, c) / num;
+    __syncthreads();
 #pragma unroll
     for (int j = 0; j < V; ++j) {
-        mu[j] = p.on ? ch[p.rel + j] / num : 0.f;
+        mu[j] = p.on ? ch[p.rel + j] : 0.f;
         s[j] = 0.f;
     }
-    each<K>(q, p, [&](int i, int64_t) {
+    each<DT, K>(q, p, [&](int i, uint32_t) {
         float f[V];
         P::open(d[i], f);
 #pragma unroll
@@ -265,60 +306,67 @@ __global__ __launch_bounds__(256) void k_gn_colparts_fwd(const typename Elt<DT>:
             s[j] = fmaf(e, e, s[j]);
         }
     });
-    channel_sums<V>(s, q, p.width, lds, ch2);
+    wave_channels<V>(s, q, p.width, lds + all);
+    __syncthreads();
     for (int c = threadIdx.x; c < p.width; c += blockDim.x)
-        parts[(int64_t(p.n) * q.c + p.c0 + c) * q.chunks + p.chunk] = make_float4(ch[c] / num, ch2[c], num, 0.f);
+        parts[(int64_t(p.n) * q.c + p.c0 + c) * q.chunks + p.chunk] =
+            make_float4(ch[c], sum_of_channel(lds + all, q, c), num, 0.f);
 }
 
-template <int DT, int V, int K>
-__global__ __launch_bounds__(256) void k_gn_colwrite_fwd(const typename Elt<DT>::T* __restrict__ x, Cols q, int images,
+template <int DT, int V, int K, int ACT>
+__global__ __launch_bounds__(256, 4) void k_gn_colwrite_fwd(const typename Elt<DT>::T* __restrict__ x, Cols q, int images,
                                                          Params w, const float* __restrict__ mean,
                                                          const float* __restrict__ rstd,
                                                          typename Elt<DT>::T* __restrict__ y) {
     using P = Pack<DT, V>;
     Place p;
     if (!place<V>(q, images, p)) return;
+    const int64_t at = base_of(q, p);
+    const typename Elt<DT>::T* xb = x + at;
     typename P::R d[K];
-    each<K>(q, p, [&](int i, int64_t at) { d[i] = get<DT, V>(x, at); });
-    Coeff<V> k;
+    each<DT, K>(q, p, [&](int i, uint32_t byte) { d[i] = get<typename P::R>(xb, byte); });
+    Coeff k[V];
     coefficients<V>(q, p, w, mean, rstd, k);
-    each<K>(q, p, [&](int i, int64_t at) {
+    each<DT, K>(q, p, [&](int i, uint32_t byte) {
         float f[V];
         P::open(d[i], f);
 #pragma unroll
-        for (int j = 0; j < V; ++j) f[j] = act_of(affine((f[j] - k.mu[j]) * k.r[j], k.ga[j], k.be[j]), w.act);
-        put<DT, V>(y, at, f);
+        for (int j = 0; j < V; ++j) f[j] = forward<ACT>(k[j], f[j]);
+        put(y + at, byte, P::close(f));
     });
 }
 
-template <int DT, int V, int K>
-__global__ __launch_bounds__(256) void k_gn_colparts_bwd(const typename Elt<DT>::T* __restrict__ x,
+template <int DT, int V, int K, int ACT>
+__global__ __launch_bounds__(256, 4) void k_gn_colparts_bwd(const typename Elt<DT>::T* __restrict__ x,
                                                          const typename Elt<DT>::T* __restrict__ dy, Cols q, int images,
                                                          Params w, const float* __restrict__ mean,
                                                          const float* __restrict__ rstd, float2* __restrict__ parts) {
     using P = Pack<DT, V>;
-    extern __shared__ float lds[];
+    extern __shared__ float lds[];              // the waves' sums, two
     Place p;
     if (!place<V>(q, images, p)) return;
-    float* ch = lds_of_channels(lds, q);
-    float* ch2 = ch + q.tile;
+    const int all = sum_rows(q) * q.tile;
+    const int64_t at = base_of(q, p);
+    const typename Elt<DT>::T *xb = x + at, *gb = dy + at;
     typename P::R d[K], e[K];
-    each<K>(q, p, [&](int i, int64_t at) {
-        d[i] = get<DT, V>(x, at);
-        e[i] = get<DT, V>(dy, at);
+    each<DT, K>(q, p, [&](int i, uint32_t byte) {
+        d[i] = get<typename P::R>(xb, byte);
+        e[i] = get<typename P::R>(gb, byte);
     });
-    Coeff<V> k;
+    Coeff k[V];
     coefficients<V>(q, p, w, mean, rstd, k);
     float a[V], b[V];
-    sums_back<DT, V, K>(d, e, q, p, k, w.act, a, b);
-    channel_sums<V>(a, q, p.width, lds, ch);
-    channel_sums<V>(b, q, p.width, lds, ch2);
+    sums_back<DT, V, K, ACT>(d, e, q, p, k, a, b);
+    wave_channels<V>(a, q, p.width, lds);
+    wave_channels<V>(b, q, p.width, lds + all);
+    __syncthreads();
     for (int c = threadIdx.x; c < p.width; c += blockDim.x)
-        parts[(int64_t(p.n) * q.c + p.c0 + c) * q.chunks + p.chunk] = make_float2(ch[c], ch2[c]);
+        parts[(int64_t(p.n) * q.c + p.c0 + c) * q.chunks + p.chunk] =
+            make_float2(sum_of_channel(lds, q, c), sum_of_channel(lds + all, q, c));
 }
 
-template <int DT, int V, int K>
-__global__ __launch_bounds__(256) void k_gn_colwrite_bwd(const typename Elt<DT>::T* __restrict__ x,
+template <int DT, int V, int K, int ACT>
+__global__ __launch_bounds__(256, 4) void k_gn_colwrite_bwd(const typename Elt<DT>::T* __restrict__ x,
                                                          const typename Elt<DT>::T* __restrict__ dy, Cols q, int images,
                                                          Params w, const float* __restrict__ mean,
                                                          const float* __restrict__ rstd, const float2* __restrict__ s12,
@@ -326,27 +374,23 @@ __global__ __launch_bounds__(256) void k_gn_colwrite_bwd(const typename Elt<DT>:
     using P = Pack<DT, V>;
     Place p;
     if (!place<V>(q, images, p)) return;
+    const int64_t at = base_of(q, p);
+    const typename Elt<DT>::T *xb = x + at, *gb = dy + at;
     typename P::R d[K], e[K];
-    each<K>(q, p, [&](int i, int64_t at) {
-        d[i] = get<DT, V>(x, at);
-        e[i] = get<DT, V>(dy, at);
+    each<DT, K>(q, p, [&](int i, uint32_t byte) {
+        d[i] = get<typename P::R>(xb, byte);
+        e[i] = get<typename P::R>(gb, byte);
     });
-    Coeff<V> k;
+    Coeff k[V];
     coefficients<V>(q, p, w, mean, rstd, k);
     float s1[V], s2[V];
 #pragma unroll
     for (int j = 0; j < V; ++j) {
         const int c = p.on ? p.c0 + p.rel + j : 0;
-        const float2 t = s12[int64_t(p.n) * q.groups + c / q.cg];
+        const float2 t = s12[int64_t(p.n) * q.groups + group_of(q, c)];
         s1[j] = t.x, s2[j] = t.y;
     }
-    write_back<DT, V, K>(d, e, q, p, k, w.act, s1, s2, dx);
-}
-
-// Bytes of LDS: `more` arrays of the tile's width behind the threads' sums.
-unsigned lds_bytes(const Plan& p, int more) {
-    const int span_log2 = p.cols.cols_log2 > 6 ? p.cols.cols_log2 : 6;
-    return unsigned(sizeof(float)) * unsigned(p.cols.tile) * unsigned((p.threads >> span_log2) + more);
+    write_back<DT, V, K, ACT>(d, e, q, p, k, s1, s2, dx + at);
 }
 
 template <int DT, int V>
@@ -357,20 +401,22 @@ void fwd(const Plan& p, int n, const void* x, const Params& q, float eps, void* 
     T* yt = static_cast<T*>(y);
     const dim3 grid(static_cast<unsigned>(p.grid)), block(static_cast<unsigned>(p.threads));
     if (p.held) {
-        const auto go = [&](auto k) {
-            hipLaunchKernelGGL((k_gn_cols_fwd<DT, V, decltype(k)::value>), grid, block, lds_bytes(p, 2), st, xt, p.cols, n,
-                               q, eps, yt, mean, rstd);
-        };
-        if (p.k <= 2) go(IntC<2>{});
-        else if (p.k <= 4) go(IntC<4>{});
-        else if (p.k <= 8) go(IntC<8>{});
-        else go(IntC<16>{});
+        with_act(q.act, [&](auto act) {
+            with_count<V, false>(p.k, [&](auto k) {
+                hipLaunchKernelGGL((k_gn_cols_fwd<DT, V, decltype(k)::value, decltype(act)::value>), grid, block,
+                                   cols_lds(p.cols, p.threads, 1, 2), st, xt, p.cols, n, q, eps, yt, mean, rstd);
+            });
+        });
         return;
     }
     constexpr int K = V == 1 ? kPieceSingle : kPiece;
-    hipLaunchKernelGGL((k_gn_colparts_fwd<DT, V, K>), grid, block, lds_bytes(p, 2), st, xt, p.cols, n, parts);
+    hipLaunchKernelGGL((k_gn_colparts_fwd<DT, V, K>), grid, block, cols_lds(p.cols, p.threads, 2, 1), st, xt, p.cols, n,
+                       parts);
     combine_fwd(parts, int64_t(n) * p.cols.groups, p.cols.cg * p.pieces, eps, mean, rstd, st);
-    hipLaunchKernelGGL((k_gn_colwrite_fwd<DT, V, K>), grid, block, 0, st, xt, p.cols, n, q, mean, rstd, yt);
+    with_act(q.act, [&](auto act) {
+        hipLaunchKernelGGL((k_gn_colwrite_fwd<DT, V, K, decltype(act)::value>), grid, block, 0, st, xt, p.cols, n, q, mean,
+                           rstd, yt);
+    });
 }
 
 template <int DT, int V>
@@ -381,21 +427,23 @@ void bwd(const Plan& p, int n, const void* x, const void* dy, const Params& q, c
     T* dt = static_cast<T*>(dx);
     const dim3 grid(static_cast<unsigned>(p.grid)), block(static_cast<unsigned>(p.threads));
     if (p.held) {
-        const auto go = [&](auto k) {
-            hipLaunchKernelGGL((k_gn_cols_bwd<DT, V, decltype(k)::value>), grid, block, lds_bytes(p, 4), st, xt, gt, p.cols,
-                               n, q, mean, rstd, dt, parts);
-        };
-        if (p.k <= 2) go(IntC<2>{});
-        else if (p.k <= 4) go(IntC<4>{});
-        else go(IntC<8>{});
+        with_act(q.act, [&](auto act) {
+            with_count<V, true>(p.k, [&](auto k) {
+                hipLaunchKernelGGL((k_gn_cols_bwd<DT, V, decltype(k)::value, decltype(act)::value>), grid, block,
+                                   cols_lds(p.cols, p.threads, 2, 4), st, xt, gt, p.cols, n, q, mean, rstd, dt, parts);
+            });
+        });
         return;
     }
     constexpr int K = V == 1 ? kPieceSingle : kPiece;
-    hipLaunchKernelGGL((k_gn_colparts_bwd<DT, V, K>), grid, block, lds_bytes(p, 2), st, xt, gt, p.cols, n, q, mean, rstd,
-                       parts);
-    combine_bwd(parts, int64_t(n) * p.cols.groups, p.cols.cg * p.pieces, p.pieces, p.cols.groups, p.cols.cg,
-                float(p.cols.cg) * float(p.cols.hw), q.gamma, s12, st);
-    hipLaunchKernelGGL((k_gn_colwrite_bwd<DT, V, K>), grid, block, 0, st, xt, gt, p.cols, n, q, mean, rstd, s12, dt);
+    with_act(q.act, [&](auto act) {
+        hipLaunchKernelGGL((k_gn_colparts_bwd<DT, V, K, decltype(act)::value>), grid, block,
+                           cols_lds(p.cols, p.threads, 2, 0), st, xt, gt, p.cols, n, q, mean, rstd, parts);
+        combine_bwd(parts, int64_t(n) * p.cols.groups, p.cols.cg * p.pieces, p.pieces, p.cols.groups, p.cols.cg,
+                    float(p.cols.cg) * float(p.cols.hw), q.gamma, s12, st);
+        hipLaunchKernelGGL((k_gn_colwrite_bwd<DT, V, K, decltype(act)::value>), grid, block, 0, st, xt, gt, p.cols, n, q,
+                           mean, rstd, s12, dt);
+    });
 }
 
 }  // namespace

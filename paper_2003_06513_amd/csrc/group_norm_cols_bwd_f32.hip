@@ -1,0 +1,9 @@
+// Group normalisation with the channels last, backward, fp32.
+#include "group_norm_cols.h"
+
+namespace psc {
+namespace gn {
+template void cols_bwd<DT_F32>(const Plan&, int, const void*, const void*, const Params&, const float*, const float*, void*,
+                               float2*, float2*, hipStream_t);
+}  // namespace gn
+}  // namespace psc

@@ -1,11 +1,9 @@
-// Group normalisation with the channels last, fp16.
+// Group normalisation with the channels last, forward, fp16.
 #include "group_norm_cols.h"
 
 namespace psc {
 namespace gn {
 template void cols_fwd<DT_F16>(const Plan&, int, const void*, const Params&, float, void*, float*, float*, float4*,
                                hipStream_t);
-template void cols_bwd<DT_F16>(const Plan&, int, const void*, const void*, const Params&, const float*, const float*,
-                               void*, float2*, float2*, hipStream_t);
 }  // namespace gn
 }  // namespace psc

@@ -8,182 +8,195 @@ namespace gn {
 namespace {
 
 // Calls f(i, row, window) for the vectors of this thread: slot i, row of the
-// group.  base: the group's first element.
-template <int V, bool MASK, int K, class F>
-__device__ __forceinline__ void each(const Rows& s, int64_t base, F f) {
+// group, and after(i, row) where the thread has done with a row.
+template <int V, bool MASK, int K, class F, class G>
+__device__ __forceinline__ void each(const Rows& s, const Base<V, MASK>& b, F f, G after) {
     const int lanes = 1 << s.lanes_log2;
-    const int lane = threadIdx.x & (lanes - 1), rows = int(blockDim.x >> s.lanes_log2);
+    const int lane = int(threadIdx.x) & (lanes - 1), rows = int(blockDim.x >> s.lanes_log2);
     int row = int(threadIdx.x >> s.lanes_log2), v = 0;
 #pragma unroll
     for (int i = 0; i < K; ++i) {
         if (i < s.slots) {
             if (row < s.cg) {
-                const Window w = window<V, MASK>(s, base + int64_t(row) * s.hw, v * lanes + lane);
+                const Window w = window<V, MASK>(b, row * s.hw, s.hw, v * lanes + lane);
                 if (w.hi > w.lo) f(i, row, w);
             }
-            if (++v == s.vi) v = 0, row += rows;
+            if (++v == s.vi) {
+                after(row);
+                v = 0, row += rows;
+            }
         }
     }
 }
+struct Nothing {
+    __device__ __forceinline__ void operator()(int) const {}
+};
 
-template <int DT, int V, bool MASK, int K>
-__global__ __launch_bounds__(K <= 4 ? 1024 : 512) void k_gn_rows_fwd(const typename Elt<DT>::T* __restrict__ x, Rows s,
-                                                                     Params q, float eps,
-                                                                     typename Elt<DT>::T* __restrict__ y,
-                                                                     float* __restrict__ mean, float* __restrict__ rstd) {
+template <int DT, int V, bool MASK, int K, int ACT>
+__global__ __launch_bounds__(threads_of(V, K)) void k_gn_rows_fwd(const typename Elt<DT>::T* __restrict__ x, Rows s,
+                                                                  Params q, float eps,
+                                                                  typename Elt<DT>::T* __restrict__ y,
+                                                                  float* __restrict__ mean, float* __restrict__ rstd) {
     using P = Pack<DT, V>;
-    __shared__ float part[16];
-    const int64_t ng = blockIdx.x, base = ng * s.cg * s.hw;
-    const int c0 = int(ng % s.groups) * s.cg;
+    __shared__ float part[32];
+    extern __shared__ float2 row_params[];      // gamma and beta of the rows
+    const Base<V, MASK> b(s, int64_t(blockIdx.x) * s.cg * s.hw);
+    const int c0 = int(blockIdx.x % unsigned(s.groups)) * s.cg;
     typename P::R d[K];
-    each<V, MASK, K>(s, base, [&](int i, int, const Window& w) { d[i] = load<DT, V, MASK>(x, w, s.total); });
+    each<V, MASK, K>(s, b, [&](int i, int, const Window& w) { d[i] = load<DT, V, MASK>(x, b, w); }, Nothing());
+    for (int row = threadIdx.x; row < s.cg; row += blockDim.x)
+        row_params[row] = make_float2(or_one(q.gamma, c0 + row), or_zero(q.beta, c0 + row));
     float sum = 0.f;
-    each<V, MASK, K>(s, base, [&](int i, int, const Window& w) {
+    each<V, MASK, K>(s, b, [&](int i, int, const Window& w) {
         float f[V];
         P::open(d[i], f);
 #pragma unroll
         for (int j = 0; j < V; ++j) sum += in<MASK>(w, j) ? f[j] : 0.f;
-    });
+    }, Nothing());
     const float m = float(s.cg) * float(s.hw);
-    const float mu = block_sum(sum, part) / m;
+    Coeff k;
+    k.mu = block_sum(sum, part) / m;
     float sq = 0.f;
-    each<V, MASK, K>(s, base, [&](int i, int, const Window& w) {
+    each<V, MASK, K>(s, b, [&](int i, int, const Window& w) {
         float f[V];
         P::open(d[i], f);
 #pragma unroll
         for (int j = 0; j < V; ++j) {
-            const float e = in<MASK>(w, j) ? f[j] - mu : 0.f;
+            const float e = in<MASK>(w, j) ? f[j] - k.mu : 0.f;
             sq = fmaf(e, e, sq);
         }
-    });
-    const float r = 1.f / sqrtf(block_sum(sq, part) / m + eps);
+    }, Nothing());
+    k.r = 1.f / sqrtf(block_sum(sq, part + 16) / m + eps);
     if (threadIdx.x == 0 && mean) {
-        mean[ng] = mu;
-        rstd[ng] = r;
+        mean[blockIdx.x] = k.mu;
+        rstd[blockIdx.x] = k.r;
     }
-    each<V, MASK, K>(s, base, [&](int i, int row, const Window& w) {
-        const float ga = or_one(q.gamma, c0 + row), be = or_zero(q.beta, c0 + row);
+    if (blockDim.x == 64) __syncthreads();      // the sums of larger blocks had one
+    each<V, MASK, K>(s, b, [&](int i, int row, const Window& w) {
+        const float2 gb = row_params[row];
+        k.ga = gb.x, k.be = gb.y;
         float f[V];
         P::open(d[i], f);
 #pragma unroll
-        for (int j = 0; j < V; ++j) f[j] = act_of(affine((f[j] - mu) * r, ga, be), q.act);
-        store<DT, V, MASK>(y, w, f);
-    });
+        for (int j = 0; j < V; ++j) f[j] = forward<ACT>(k, f[j]);
+        store<DT, V, MASK>(y, b, w, f);
+    }, Nothing());
 }
 
 // sums [n][c]: A and B of each row, for the parameters' gradients; may be NULL.
-template <int DT, int V, bool MASK, int K>
-__global__ __launch_bounds__(K <= 4 ? 1024 : 512) void k_gn_rows_bwd(const typename Elt<DT>::T* __restrict__ x,
-                                                                     const typename Elt<DT>::T* __restrict__ dy, Rows s,
-                                                                     Params q, const float* __restrict__ mean,
-                                                                     const float* __restrict__ rstd,
-                                                                     typename Elt<DT>::T* __restrict__ dx,
-                                                                     float2* __restrict__ sums) {
+template <int DT, int V, bool MASK, int K, int ACT>
+__global__ __launch_bounds__(threads_of(V, K)) void k_gn_rows_bwd(const typename Elt<DT>::T* __restrict__ x,
+                                                                  const typename Elt<DT>::T* __restrict__ dy, Rows s,
+                                                                  Params q, const float* __restrict__ mean,
+                                                                  const float* __restrict__ rstd,
+                                                                  typename Elt<DT>::T* __restrict__ dx,
+                                                                  float2* __restrict__ sums) {
     using P = Pack<DT, V>;
-    extern __shared__ float2 row_parts[];       // [cg][waves that share a row]
-    __shared__ float part[16];
-    const int64_t ng = blockIdx.x, base = ng * s.cg * s.hw;
-    const int c0 = int(ng % s.groups) * s.cg;
-    const float mu = mean[ng], r = rstd[ng];
+    extern __shared__ float2 row_params[];      // gamma and beta of the rows
+    float2* row_parts = row_params + s.cg;      // [cg][waves that share a row]
+    __shared__ float part[32];
+    const Base<V, MASK> b(s, int64_t(blockIdx.x) * s.cg * s.hw);
+    const int c0 = int(blockIdx.x % unsigned(s.groups)) * s.cg;
+    Coeff k;
+    k.mu = mean[blockIdx.x], k.r = rstd[blockIdx.x];
     typename P::R d[K], e[K];
-    each<V, MASK, K>(s, base, [&](int i, int, const Window& w) {
-        d[i] = load<DT, V, MASK>(x, w, s.total);
-        e[i] = load<DT, V, MASK>(dy, w, s.total);
-    });
-    const int lanes = 1 << s.lanes_log2, lane = threadIdx.x & (lanes - 1);
-    const int share = lanes > 64 ? lanes >> 6 : 1;
-    {
-        const int rows = int(blockDim.x >> s.lanes_log2);
-        int row = int(threadIdx.x >> s.lanes_log2), v = 0;
-        float a = 0.f, b = 0.f;
-#pragma unroll
-        for (int i = 0; i < K; ++i) {
-            if (i < s.slots) {
-                if (row < s.cg) {
-                    const Window w = window<V, MASK>(s, base + int64_t(row) * s.hw, v * lanes + lane);
-                    if (w.hi > w.lo) {
-                        const float ga = or_one(q.gamma, c0 + row), be = or_zero(q.beta, c0 + row);
-                        float f[V], g[V];
-                        P::open(d[i], f);
-                        P::open(e[i], g);
-#pragma unroll
-                        for (int j = 0; j < V; ++j) {
-                            const float xh = (f[j] - mu) * r;
-                            const float du = in<MASK>(w, j) ? act_back(affine(xh, ga, be), g[j], q.act) : 0.f;
-                            a += du;
-                            b = in<MASK>(w, j) ? fmaf(du, xh, b) : b;
-                        }
-                    }
-                }
-                if (++v == s.vi) {
-                    for (int off = 1; off < lanes && off < 64; off <<= 1) {
-                        a += __shfl_xor(a, off);
-                        b += __shfl_xor(b, off);
-                    }
-                    if (row < s.cg && (lane & 63) == 0) row_parts[row * share + (lane >> 6)] = make_float2(a, b);
-                    a = 0.f, b = 0.f;
-                    v = 0, row += rows;
-                }
-            }
-        }
-    }
+    each<V, MASK, K>(s, b, [&](int i, int, const Window& w) {
+        d[i] = load<DT, V, MASK>(x, b, w);
+        e[i] = load<DT, V, MASK>(dy, b, w);
+    }, Nothing());
+    for (int row = threadIdx.x; row < s.cg; row += blockDim.x)
+        row_params[row] = make_float2(or_one(q.gamma, c0 + row), or_zero(q.beta, c0 + row));
     __syncthreads();
-    float s1 = 0.f, s2 = 0.f;
-    for (int row = threadIdx.x; row < s.cg; row += blockDim.x) {
-        float a = 0.f, b = 0.f;
-        for (int i = 0; i < share; ++i) {
-            const float2 ab = row_parts[row * share + i];
-            a += ab.x;
-            b += ab.y;
-        }
-        if (sums) sums[ng * s.cg + row] = make_float2(a, b);
-        const float ga = or_one(q.gamma, c0 + row);
-        s1 = fmaf(ga, a, s1);
-        s2 = fmaf(ga, b, s2);
-    }
-    const float m = float(s.cg) * float(s.hw);
-    s1 = block_sum(s1, part) / m;
-    s2 = block_sum(s2, part) / m;
-    each<V, MASK, K>(s, base, [&](int i, int row, const Window& w) {
-        const float ga = or_one(q.gamma, c0 + row), be = or_zero(q.beta, c0 + row);
+    const int lanes = 1 << s.lanes_log2, lane = int(threadIdx.x) & (lanes - 1);
+    const int share = lanes > 64 ? lanes >> 6 : 1;
+    float sa = 0.f, sb = 0.f;
+    each<V, MASK, K>(s, b, [&](int i, int row, const Window& w) {
+        const float2 gb = row_params[row];
+        k.ga = gb.x, k.be = gb.y;
         float f[V], g[V];
         P::open(d[i], f);
         P::open(e[i], g);
 #pragma unroll
         for (int j = 0; j < V; ++j) {
-            const float xh = (f[j] - mu) * r;
-            const float du = act_back(affine(xh, ga, be), g[j], q.act);
-            f[j] = r * (fmaf(ga, du, -s1) - xh * s2);
+            const float xh = normal(k, f[j]);
+            const float du = in<MASK>(w, j) ? slope<ACT>(k, xh, g[j]) : 0.f;
+            sa += du;
+            sb = in<MASK>(w, j) ? fmaf(du, xh, sb) : sb;
         }
-        store<DT, V, MASK>(dx, w, f);
+    }, [&](int row) {
+        sa = run_sum(sa, lanes);
+        sb = run_sum(sb, lanes);
+        if (row < s.cg && (lane & 63) == 0) row_parts[row * share + (lane >> 6)] = make_float2(sa, sb);
+        sa = 0.f, sb = 0.f;
     });
+    __syncthreads();
+    float s1 = 0.f, s2 = 0.f;
+    for (int row = threadIdx.x; row < s.cg; row += blockDim.x) {
+        float a = 0.f, c = 0.f;
+        for (int i = 0; i < share; ++i) {
+            const float2 t = row_parts[row * share + i];
+            a += t.x;
+            c += t.y;
+        }
+        if (sums) sums[int64_t(blockIdx.x) * s.cg + row] = make_float2(a, c);
+        const float ga = row_params[row].x;
+        s1 = fmaf(ga, a, s1);
+        s2 = fmaf(ga, c, s2);
+    }
+    const float m = float(s.cg) * float(s.hw);
+    const float2 both = block_sum2(s1, s2, part);
+    s1 = both.x / m, s2 = both.y / m;
+    each<V, MASK, K>(s, b, [&](int i, int row, const Window& w) {
+        const float2 gb = row_params[row];
+        k.ga = gb.x, k.be = gb.y;
+        float f[V], g[V];
+        P::open(d[i], f);
+        P::open(e[i], g);
+#pragma unroll
+        for (int j = 0; j < V; ++j) f[j] = backward<ACT>(k, f[j], g[j], s1, s2);
+        store<DT, V, MASK>(dx, b, w, f);
+    }, Nothing());
 }
 
 // ---- pieces: a wave takes K x 64 vectors of a row.
 
+struct Piece {
+    unsigned id, row, ng;
+    int c, piece;
+};
+__device__ __forceinline__ Piece piece_of(const Rows& s, int pieces) {
+    Piece p;
+    p.id = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6));
+    p.row = p.id / unsigned(pieces);
+    p.piece = int(p.id - p.row * unsigned(pieces));
+    p.ng = p.row / unsigned(s.cg);
+    p.c = int(p.row % unsigned(s.cg * s.groups));
+    return p;
+}
+// Calls f(i, window): the windows of a row from `skip` vectors on.
 template <int V, bool MASK, int K, class F>
-__device__ __forceinline__ void each_of_piece(const Rows& s, int64_t at, int piece, F f) {
-    const int lane = threadIdx.x & 63;
+__device__ __forceinline__ void each_of_piece(const Rows& s, const Base<V, MASK>& b, int skip, F f) {
+    const int lane = int(threadIdx.x & 63);
 #pragma unroll
     for (int i = 0; i < K; ++i) {
-        const Window w = window<V, MASK>(s, at, (piece * K + i) * 64 + lane);
+        const Window w = window<V, MASK>(b, 0, s.hw, skip + i * 64 + lane);
         if (w.hi > w.lo) f(i, w);
     }
 }
 
-// The number of elements, their mean and their squares about it.
+// The mean of the elements, their squares about it, and their number.
 template <int DT, int V, bool MASK, int K>
-__global__ __launch_bounds__(256) void k_gn_rowparts_fwd(const typename Elt<DT>::T* __restrict__ x, Rows s, int pieces,
-                                                         int64_t count, float4* __restrict__ parts) {
+__global__ __launch_bounds__(256, 4) void k_gn_rowparts_fwd(const typename Elt<DT>::T* __restrict__ x, Rows s, int pieces,
+                                                         unsigned count, float4* __restrict__ parts) {
     using P = Pack<DT, V>;
-    const int64_t id = int64_t(blockIdx.x) * 4 + (threadIdx.x >> 6);
-    if (id >= count) return;
-    const int64_t at = id / pieces * s.hw;
-    const int piece = int(id % pieces);
+    const Piece p = piece_of(s, pieces);
+    if (p.id >= count) return;
+    const Base<V, MASK> b(s, int64_t(p.row) * s.hw);
+    const int skip = p.piece * K * 64;
     typename P::R d[K];
-    each_of_piece<V, MASK, K>(s, at, piece, [&](int i, const Window& w) { d[i] = load<DT, V, MASK>(x, w, s.total); });
+    each_of_piece<V, MASK, K>(s, b, skip, [&](int i, const Window& w) { d[i] = load<DT, V, MASK>(x, b, w); });
     float sum = 0.f, num = 0.f;
-    each_of_piece<V, MASK, K>(s, at, piece, [&](int i, const Window& w) {
+    each_of_piece<V, MASK, K>(s, b, skip, [&](int i, const Window& w) {
         float f[V];
         P::open(d[i], f);
         num += float(w.hi - w.lo);
@@ -193,7 +206,7 @@ __global__ __launch_bounds__(256) void k_gn_rowparts_fwd(const typename Elt<DT>:
     num = wave_sum(num);
     const float mu = num > 0.f ? wave_sum(sum) / num : 0.f;
     float sq = 0.f;
-    each_of_piece<V, MASK, K>(s, at, piece, [&](int i, const Window& w) {
+    each_of_piece<V, MASK, K>(s, b, skip, [&](int i, const Window& w) {
         float f[V];
         P::open(d[i], f);
 #pragma unroll
@@ -203,100 +216,94 @@ __global__ __launch_bounds__(256) void k_gn_rowparts_fwd(const typename Elt<DT>:
         }
     });
     sq = wave_sum(sq);
-    if ((threadIdx.x & 63) == 0) parts[id] = make_float4(mu, sq, num, 0.f);
+    if ((threadIdx.x & 63) == 0) parts[p.id] = make_float4(mu, sq, num, 0.f);
 }
 
-template <int DT, int V, bool MASK, int K>
-__global__ __launch_bounds__(256) void k_gn_rowwrite_fwd(const typename Elt<DT>::T* __restrict__ x, Rows s, Params q,
-                                                         int pieces, int64_t count, const float* __restrict__ mean,
+__device__ __forceinline__ Coeff coeff_of(const Piece& p, const Params& q, const float* mean, const float* rstd) {
+    return Coeff{mean[p.ng], rstd[p.ng], or_one(q.gamma, p.c), or_zero(q.beta, p.c)};
+}
+
+template <int DT, int V, bool MASK, int K, int ACT>
+__global__ __launch_bounds__(256, 4) void k_gn_rowwrite_fwd(const typename Elt<DT>::T* __restrict__ x, Rows s, Params q,
+                                                         int pieces, unsigned count, const float* __restrict__ mean,
                                                          const float* __restrict__ rstd,
                                                          typename Elt<DT>::T* __restrict__ y) {
     using P = Pack<DT, V>;
-    const int64_t id = int64_t(blockIdx.x) * 4 + (threadIdx.x >> 6);
-    if (id >= count) return;
-    const int64_t row = id / pieces, at = row * s.hw;
-    const int piece = int(id % pieces);
-    const int64_t ng = row / s.cg;
-    const int c = int(row % (int64_t(s.cg) * s.groups));
+    const Piece p = piece_of(s, pieces);
+    if (p.id >= count) return;
+    const Base<V, MASK> b(s, int64_t(p.row) * s.hw);
+    const int skip = p.piece * K * 64;
     typename P::R d[K];
-    each_of_piece<V, MASK, K>(s, at, piece, [&](int i, const Window& w) { d[i] = load<DT, V, MASK>(x, w, s.total); });
-    const float mu = mean[ng], r = rstd[ng], ga = or_one(q.gamma, c), be = or_zero(q.beta, c);
-    each_of_piece<V, MASK, K>(s, at, piece, [&](int i, const Window& w) {
+    each_of_piece<V, MASK, K>(s, b, skip, [&](int i, const Window& w) { d[i] = load<DT, V, MASK>(x, b, w); });
+    const Coeff k = coeff_of(p, q, mean, rstd);
+    each_of_piece<V, MASK, K>(s, b, skip, [&](int i, const Window& w) {
         float f[V];
         P::open(d[i], f);
 #pragma unroll
-        for (int j = 0; j < V; ++j) f[j] = act_of(affine((f[j] - mu) * r, ga, be), q.act);
-        store<DT, V, MASK>(y, w, f);
+        for (int j = 0; j < V; ++j) f[j] = forward<ACT>(k, f[j]);
+        store<DT, V, MASK>(y, b, w, f);
     });
 }
 
-template <int DT, int V, bool MASK, int K>
-__global__ __launch_bounds__(256) void k_gn_rowparts_bwd(const typename Elt<DT>::T* __restrict__ x,
+template <int DT, int V, bool MASK, int K, int ACT>
+__global__ __launch_bounds__(256, 4) void k_gn_rowparts_bwd(const typename Elt<DT>::T* __restrict__ x,
                                                          const typename Elt<DT>::T* __restrict__ dy, Rows s, Params q,
-                                                         int pieces, int64_t count, const float* __restrict__ mean,
+                                                         int pieces, unsigned count, const float* __restrict__ mean,
                                                          const float* __restrict__ rstd, float2* __restrict__ parts) {
     using P = Pack<DT, V>;
-    const int64_t id = int64_t(blockIdx.x) * 4 + (threadIdx.x >> 6);
-    if (id >= count) return;
-    const int64_t row = id / pieces, at = row * s.hw;
-    const int piece = int(id % pieces);
-    const int64_t ng = row / s.cg;
-    const int c = int(row % (int64_t(s.cg) * s.groups));
+    const Piece p = piece_of(s, pieces);
+    if (p.id >= count) return;
+    const Base<V, MASK> b(s, int64_t(p.row) * s.hw);
+    const int skip = p.piece * K * 64;
     typename P::R d[K], e[K];
-    each_of_piece<V, MASK, K>(s, at, piece, [&](int i, const Window& w) {
-        d[i] = load<DT, V, MASK>(x, w, s.total);
-        e[i] = load<DT, V, MASK>(dy, w, s.total);
+    each_of_piece<V, MASK, K>(s, b, skip, [&](int i, const Window& w) {
+        d[i] = load<DT, V, MASK>(x, b, w);
+        e[i] = load<DT, V, MASK>(dy, b, w);
     });
-    const float mu = mean[ng], r = rstd[ng], ga = or_one(q.gamma, c), be = or_zero(q.beta, c);
-    float a = 0.f, b = 0.f;
-    each_of_piece<V, MASK, K>(s, at, piece, [&](int i, const Window& w) {
+    const Coeff k = coeff_of(p, q, mean, rstd);
+    float sa = 0.f, sb = 0.f;
+    each_of_piece<V, MASK, K>(s, b, skip, [&](int i, const Window& w) {
         float f[V], g[V];
         P::open(d[i], f);
         P::open(e[i], g);
 #pragma unroll
         for (int j = 0; j < V; ++j) {
-            const float xh = (f[j] - mu) * r;
-            const float du = in<MASK>(w, j) ? act_back(affine(xh, ga, be), g[j], q.act) : 0.f;
-            a += du;
-            b = in<MASK>(w, j) ? fmaf(du, xh, b) : b;
+            const float xh = normal(k, f[j]);
+            const float du = in<MASK>(w, j) ? slope<ACT>(k, xh, g[j]) : 0.f;
+            sa += du;
+            sb = in<MASK>(w, j) ? fmaf(du, xh, sb) : sb;
         }
     });
-    a = wave_sum(a);
-    b = wave_sum(b);
-    if ((threadIdx.x & 63) == 0) parts[id] = make_float2(a, b);
+    sa = wave_sum(sa);
+    sb = wave_sum(sb);
+    if ((threadIdx.x & 63) == 0) parts[p.id] = make_float2(sa, sb);
 }
 
-template <int DT, int V, bool MASK, int K>
-__global__ __launch_bounds__(256) void k_gn_rowwrite_bwd(const typename Elt<DT>::T* __restrict__ x,
+template <int DT, int V, bool MASK, int K, int ACT>
+__global__ __launch_bounds__(256, 4) void k_gn_rowwrite_bwd(const typename Elt<DT>::T* __restrict__ x,
                                                          const typename Elt<DT>::T* __restrict__ dy, Rows s, Params q,
-                                                         int pieces, int64_t count, const float* __restrict__ mean,
+                                                         int pieces, unsigned count, const float* __restrict__ mean,
                                                          const float* __restrict__ rstd, const float2* __restrict__ s12,
                                                          typename Elt<DT>::T* __restrict__ dx) {
     using P = Pack<DT, V>;
-    const int64_t id = int64_t(blockIdx.x) * 4 + (threadIdx.x >> 6);
-    if (id >= count) return;
-    const int64_t row = id / pieces, at = row * s.hw;
-    const int piece = int(id % pieces);
-    const int64_t ng = row / s.cg;
-    const int c = int(row % (int64_t(s.cg) * s.groups));
+    const Piece p = piece_of(s, pieces);
+    if (p.id >= count) return;
+    const Base<V, MASK> b(s, int64_t(p.row) * s.hw);
+    const int skip = p.piece * K * 64;
     typename P::R d[K], e[K];
-    each_of_piece<V, MASK, K>(s, at, piece, [&](int i, const Window& w) {
-        d[i] = load<DT, V, MASK>(x, w, s.total);
-        e[i] = load<DT, V, MASK>(dy, w, s.total);
+    each_of_piece<V, MASK, K>(s, b, skip, [&](int i, const Window& w) {
+        d[i] = load<DT, V, MASK>(x, b, w);
+        e[i] = load<DT, V, MASK>(dy, b, w);
     });
-    const float mu = mean[ng], r = rstd[ng], ga = or_one(q.gamma, c), be = or_zero(q.beta, c);
-    const float2 sum = s12[ng];
-    each_of_piece<V, MASK, K>(s, at, piece, [&](int i, const Window& w) {
+    const Coeff k = coeff_of(p, q, mean, rstd);
+    const float2 sum = s12[p.ng];
+    each_of_piece<V, MASK, K>(s, b, skip, [&](int i, const Window& w) {
         float f[V], g[V];
         P::open(d[i], f);
         P::open(e[i], g);
 #pragma unroll
-        for (int j = 0; j < V; ++j) {
-            const float xh = (f[j] - mu) * r;
-            const float du = act_back(affine(xh, ga, be), g[j], q.act);
-            f[j] = r * (fmaf(ga, du, -sum.x) - xh * sum.y);
-        }
-        store<DT, V, MASK>(dx, w, f);
+        for (int j = 0; j < V; ++j) f[j] = backward<ACT>(k, f[j], g[j], sum.x, sum.y);
+        store<DT, V, MASK>(dx, b, w, f);
     });
 }
 
@@ -306,24 +313,27 @@ void fwd(const Plan& p, int64_t count, const void* x, const Params& q, float eps
     using T = typename Elt<DT>::T;
     const T* xt = static_cast<const T*>(x);
     T* yt = static_cast<T*>(y);
-    if (p.held) {
-        const dim3 grid(static_cast<unsigned>(p.grid)), block(static_cast<unsigned>(p.threads));
-        const auto go = [&](auto k) {
-            hipLaunchKernelGGL((k_gn_rows_fwd<DT, V, MASK, decltype(k)::value>), grid, block, 0, st, xt, p.rows, q, eps, yt,
-                               mean, rstd);
-        };
-        if (p.k <= 2) go(IntC<2>{});
-        else if (p.k <= 4) go(IntC<4>{});
-        else if (p.k <= 8) go(IntC<8>{});
-        else go(IntC<16>{});
-        return;
-    }
+    if constexpr (V > 1)
+        if (p.held) {
+            const dim3 grid(static_cast<unsigned>(p.grid)), block(static_cast<unsigned>(p.threads));
+            const unsigned lds = unsigned(sizeof(float2)) * unsigned(p.rows.cg);
+            with_act(q.act, [&](auto act) {
+                with_count<V, false>(p.k, [&](auto k) {
+                    hipLaunchKernelGGL((k_gn_rows_fwd<DT, V, MASK, decltype(k)::value, decltype(act)::value>), grid, block,
+                                       lds, st, xt, p.rows, q, eps, yt, mean, rstd);
+                });
+            });
+            return;
+        }
     constexpr int K = V == 1 ? kPieceSingle : kPiece;
     const dim3 grid(static_cast<unsigned>((count + 3) / 4));
-    hipLaunchKernelGGL((k_gn_rowparts_fwd<DT, V, MASK, K>), grid, dim3(256), 0, st, xt, p.rows, p.pieces, count, parts);
+    hipLaunchKernelGGL((k_gn_rowparts_fwd<DT, V, MASK, K>), grid, dim3(256), 0, st, xt, p.rows, p.pieces, unsigned(count),
+                       parts);
     combine_fwd(parts, count / (int64_t(p.rows.cg) * p.pieces), p.rows.cg * p.pieces, eps, mean, rstd, st);
-    hipLaunchKernelGGL((k_gn_rowwrite_fwd<DT, V, MASK, K>), grid, dim3(256), 0, st, xt, p.rows, q, p.pieces, count, mean,
-                       rstd, yt);
+    with_act(q.act, [&](auto act) {
+        hipLaunchKernelGGL((k_gn_rowwrite_fwd<DT, V, MASK, K, decltype(act)::value>), grid, dim3(256), 0, st, xt, p.rows, q,
+                           p.pieces, unsigned(count), mean, rstd, yt);
+    });
 }
 
 template <int DT, int V, bool MASK>
@@ -332,28 +342,30 @@ void bwd(const Plan& p, int64_t count, const void* x, const void* dy, const Para
     using T = typename Elt<DT>::T;
     const T *xt = static_cast<const T*>(x), *gt = static_cast<const T*>(dy);
     T* dt = static_cast<T*>(dx);
-    if (p.held) {
-        const dim3 grid(static_cast<unsigned>(p.grid)), block(static_cast<unsigned>(p.threads));
-        const int lanes = 1 << p.rows.lanes_log2;
-        const unsigned lds = unsigned(sizeof(float2)) * unsigned(p.rows.cg) * unsigned(lanes > 64 ? lanes / 64 : 1);
-        const auto go = [&](auto k) {
-            hipLaunchKernelGGL((k_gn_rows_bwd<DT, V, MASK, decltype(k)::value>), grid, block, lds, st, xt, gt, p.rows, q,
-                               mean, rstd, dt, parts);
-        };
-        if (p.k <= 2) go(IntC<2>{});
-        else if (p.k <= 4) go(IntC<4>{});
-        else go(IntC<8>{});
-        return;
-    }
+    if constexpr (V > 1)
+        if (p.held) {
+            const dim3 grid(static_cast<unsigned>(p.grid)), block(static_cast<unsigned>(p.threads));
+            const int lanes = 1 << p.rows.lanes_log2;
+            const unsigned lds = unsigned(sizeof(float2)) * unsigned(p.rows.cg) * unsigned(1 + (lanes > 64 ? lanes / 64 : 1));
+            with_act(q.act, [&](auto act) {
+                with_count<V, true>(p.k, [&](auto k) {
+                    hipLaunchKernelGGL((k_gn_rows_bwd<DT, V, MASK, decltype(k)::value, decltype(act)::value>), grid, block,
+                                       lds, st, xt, gt, p.rows, q, mean, rstd, dt, parts);
+                });
+            });
+            return;
+        }
     constexpr int K = V == 1 ? kPieceSingle : kPiece;
     const dim3 grid(static_cast<unsigned>((count + 3) / 4));
-    hipLaunchKernelGGL((k_gn_rowparts_bwd<DT, V, MASK, K>), grid, dim3(256), 0, st, xt, gt, p.rows, q, p.pieces, count,
-                       mean, rstd, parts);
-    const float m = float(p.rows.cg) * float(p.rows.hw);
-    combine_bwd(parts, count / (int64_t(p.rows.cg) * p.pieces), p.rows.cg * p.pieces, p.pieces, p.rows.groups, p.rows.cg,
-                m, q.gamma, s12, st);
-    hipLaunchKernelGGL((k_gn_rowwrite_bwd<DT, V, MASK, K>), grid, dim3(256), 0, st, xt, gt, p.rows, q, p.pieces, count,
-                       mean, rstd, s12, dt);
+    with_act(q.act, [&](auto act) {
+        hipLaunchKernelGGL((k_gn_rowparts_bwd<DT, V, MASK, K, decltype(act)::value>), grid, dim3(256), 0, st, xt, gt,
+                           p.rows, q, p.pieces, unsigned(count), mean, rstd, parts);
+        const float m = float(p.rows.cg) * float(p.rows.hw);
+        combine_bwd(parts, count / (int64_t(p.rows.cg) * p.pieces), p.rows.cg * p.pieces, p.pieces, p.rows.groups,
+                    p.rows.cg, m, q.gamma, s12, st);
+        hipLaunchKernelGGL((k_gn_rowwrite_bwd<DT, V, MASK, K, decltype(act)::value>), grid, dim3(256), 0, st, xt, gt,
+                           p.rows, q, p.pieces, unsigned(count), mean, rstd, s12, dt);
+    });
 }
 
 }  // namespace

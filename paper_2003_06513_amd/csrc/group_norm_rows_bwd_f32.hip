@@ -1,0 +1,9 @@
+// Group normalisation in NCHW, backward, fp32.
+#include "group_norm_rows.h"
+
+namespace psc {
+namespace gn {
+template void rows_bwd<DT_F32>(const Plan&, int64_t, const void*, const void*, const Params&, const float*, const float*, void*,
+                               float2*, float2*, hipStream_t);
+}  // namespace gn
+}  // namespace psc

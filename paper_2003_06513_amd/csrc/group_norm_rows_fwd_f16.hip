@@ -1,11 +1,9 @@
-// Group normalisation in NCHW, fp16.
+// Group normalisation in NCHW, forward, fp16.
 #include "group_norm_rows.h"
 
 namespace psc {
 namespace gn {
 template void rows_fwd<DT_F16>(const Plan&, int64_t, const void*, const Params&, float, void*, float*, float*, float4*,
                                hipStream_t);
-template void rows_bwd<DT_F16>(const Plan&, int64_t, const void*, const void*, const Params&, const float*, const float*,
-                               void*, float2*, float2*, hipStream_t);
 }  // namespace gn
 }  // namespace psc
