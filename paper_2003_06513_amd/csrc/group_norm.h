@@ -206,14 +206,18 @@ template <int V, bool MASK> struct Base {
 struct Window {
     int from, lo, hi;
 };
-// Vector k of the row that begins `row` elements behind the base's `first` and has `len` elements.
+// Whether vector k of the row of `len` elements that begins `row` elements behind the base's `first` has any of it.
+template <int V, bool MASK>
+__device__ __forceinline__ bool has(const Base<V, MASK>& b, int row, int len, int k) {
+    return k * V < len + (MASK ? (b.phase + row) & (V - 1) : 0);
+}
 template <int V, bool MASK>
 __device__ __forceinline__ Window window(const Base<V, MASK>& b, int row, int len, int k) {
     Window w;
     if (!MASK) {
         w.from = row + k * V;
         w.lo = 0;
-        w.hi = k * V < len ? V : 0;
+        w.hi = V;
     } else {
         const int at = b.phase + row, phase = at & (V - 1);
         w.from = at - phase + k * V;
@@ -223,16 +227,31 @@ __device__ __forceinline__ Window window(const Base<V, MASK>& b, int row, int le
     }
     return w;
 }
+// Sixteen bytes moved by an element: to higher places, `e` in the lowest; to lower ones.
+template <int BITS> __device__ __forceinline__ u4 shifted_up(const u4& r, uint32_t e) {
+    if constexpr (BITS == 32) return u4{e, r.x, r.y, r.z};
+    else return u4{r.x << 16 | e, r.y << 16 | r.x >> 16, r.z << 16 | r.y >> 16, r.w << 16 | r.z >> 16};
+}
+template <int BITS> __device__ __forceinline__ u4 shifted_down(const u4& r) {
+    if constexpr (BITS == 32) return u4{r.y, r.z, r.w, 0};
+    else return u4{r.x >> 16 | r.y << 16, r.y >> 16 | r.z << 16, r.z >> 16 | r.w << 16, r.w >> 16};
+}
 template <int DT, int V, bool MASK>
 __device__ __forceinline__ typename Pack<DT, V>::R load(const typename Elt<DT>::T* p, const Base<V, MASK>& b, const Window& w) {
     using T = typename Elt<DT>::T;
     // the elements beside the row's are other rows', or there are none: nothing outside the tensor is read
     if (!MASK || (w.from >= b.lo && w.from + V <= b.hi))
         return get<typename Pack<DT, V>::R>(p + b.at, uint32_t(w.from) * uint32_t(sizeof(T)));
-    float f[V];
-#pragma unroll
-    for (int j = 0; j < V; ++j) f[j] = j >= w.lo && j < w.hi ? Elt<DT>::load(p, b.at + w.from + j) : 0.f;
-    return Pack<DT, V>::close(f);
+    if constexpr (MASK) {
+        // rare and small: element by element, each moved up as the next comes
+        u4 r = {0, 0, 0, 0};
+#pragma unroll 1
+        for (int j = V - 1; j >= 0; --j) {
+            const uint32_t e = j >= w.lo && j < w.hi ? uint32_t(reinterpret_cast<const typename Elt<DT>::Bits*>(p + b.at)[w.from + j]) : 0u;
+            r = shifted_up<8 * sizeof(T)>(r, e);
+        }
+        return r;
+    }
 }
 template <int DT, int V, bool MASK>
 __device__ __forceinline__ void store(typename Elt<DT>::T* p, const Base<V, MASK>& b, const Window& w, const float (&f)[V]) {
@@ -243,10 +262,14 @@ __device__ __forceinline__ void store(typename Elt<DT>::T* p, const Base<V, MASK
         put(p + b.at, byte, r);
         return;
     }
-    const T* e = reinterpret_cast<const T*>(&r);
-#pragma unroll
-    for (int j = 0; j < V; ++j)
-        if (j >= w.lo && j < w.hi) put(p + b.at, byte + j * uint32_t(sizeof(T)), e[j]);
+    if constexpr (MASK) {
+        u4 e = r;
+#pragma unroll 1
+        for (int j = 0; j < w.hi; ++j) {
+            if (j >= w.lo) put(p + b.at, byte + j * uint32_t(sizeof(T)), typename Elt<DT>::Bits(e.x));
+            e = shifted_down<8 * sizeof(T)>(e);
+        }
+    }
 }
 template <bool MASK> __device__ __forceinline__ bool in(const Window& w, int j) { return !MASK || (j >= w.lo && j < w.hi); }
 

@@ -7,8 +7,11 @@ namespace psc {
 namespace gn {
 namespace {
 
-// Calls f(i, row, window) for the vectors of this thread: slot i, row of the
-// group, and after(i, row) where the thread has done with a row.
+// Calls f(i, row, window, on) for the vectors of this thread: slot i, row of
+// the group, and after(row) where the thread has done with a row.  Where a
+// slot has nothing (not on) it is given the group's first vector: branches
+// around every slot cost more than a load that all such lanes share (compiled
+// with them, the kernels of pieces took 400 registers).
 template <int V, bool MASK, int K, class F, class G>
 __device__ __forceinline__ void each(const Rows& s, const Base<V, MASK>& b, F f, G after) {
     const int lanes = 1 << s.lanes_log2;
@@ -17,10 +20,10 @@ __device__ __forceinline__ void each(const Rows& s, const Base<V, MASK>& b, F f,
 #pragma unroll
     for (int i = 0; i < K; ++i) {
         if (i < s.slots) {
-            if (row < s.cg) {
-                const Window w = window<V, MASK>(b, row * s.hw, s.hw, v * lanes + lane);
-                if (w.hi > w.lo) f(i, row, w);
-            }
+            const int k = v * lanes + lane;
+            const bool on = row < s.cg && has<V, MASK>(b, row * s.hw, s.hw, k);
+            const int r = on ? row : 0;
+            f(i, r, window<V, MASK>(b, r * s.hw, s.hw, on ? k : 0), on);
             if (++v == s.vi) {
                 after(row);
                 v = 0, row += rows;
@@ -43,28 +46,30 @@ __global__ __launch_bounds__(threads_of(V, K)) void k_gn_rows_fwd(const typename
     const Base<V, MASK> b(s, int64_t(blockIdx.x) * s.cg * s.hw);
     const int c0 = int(blockIdx.x % unsigned(s.groups)) * s.cg;
     typename P::R d[K];
-    each<V, MASK, K>(s, b, [&](int i, int, const Window& w) { d[i] = load<DT, V, MASK>(x, b, w); }, Nothing());
+    each<V, MASK, K>(s, b, [&](int i, int, const Window& w, bool) { d[i] = load<DT, V, MASK>(x, b, w); }, Nothing());
     for (int row = threadIdx.x; row < s.cg; row += blockDim.x)
         row_params[row] = make_float2(or_one(q.gamma, c0 + row), or_zero(q.beta, c0 + row));
     float sum = 0.f;
-    each<V, MASK, K>(s, b, [&](int i, int, const Window& w) {
-        float f[V];
+    each<V, MASK, K>(s, b, [&](int i, int, const Window& w, bool on) {
+        float f[V], t = 0.f;
         P::open(d[i], f);
 #pragma unroll
-        for (int j = 0; j < V; ++j) sum += in<MASK>(w, j) ? f[j] : 0.f;
+        for (int j = 0; j < V; ++j) t += in<MASK>(w, j) ? f[j] : 0.f;
+        sum += on ? t : 0.f;
     }, Nothing());
     const float m = float(s.cg) * float(s.hw);
     Coeff k;
     k.mu = block_sum(sum, part) / m;
     float sq = 0.f;
-    each<V, MASK, K>(s, b, [&](int i, int, const Window& w) {
-        float f[V];
+    each<V, MASK, K>(s, b, [&](int i, int, const Window& w, bool on) {
+        float f[V], t = 0.f;
         P::open(d[i], f);
 #pragma unroll
         for (int j = 0; j < V; ++j) {
             const float e = in<MASK>(w, j) ? f[j] - k.mu : 0.f;
-            sq = fmaf(e, e, sq);
+            t = fmaf(e, e, t);
         }
+        sq += on ? t : 0.f;
     }, Nothing());
     k.r = 1.f / sqrtf(block_sum(sq, part + 16) / m + eps);
     if (threadIdx.x == 0 && mean) {
@@ -72,14 +77,14 @@ __global__ __launch_bounds__(threads_of(V, K)) void k_gn_rows_fwd(const typename
         rstd[blockIdx.x] = k.r;
     }
     if (blockDim.x == 64) __syncthreads();      // the sums of larger blocks had one
-    each<V, MASK, K>(s, b, [&](int i, int row, const Window& w) {
+    each<V, MASK, K>(s, b, [&](int i, int row, const Window& w, bool on) {
         const float2 gb = row_params[row];
         k.ga = gb.x, k.be = gb.y;
         float f[V];
         P::open(d[i], f);
 #pragma unroll
         for (int j = 0; j < V; ++j) f[j] = forward<ACT>(k, f[j]);
-        store<DT, V, MASK>(y, b, w, f);
+        if (on) store<DT, V, MASK>(y, b, w, f);
     }, Nothing());
 }
 
@@ -100,7 +105,7 @@ __global__ __launch_bounds__(threads_of(V, K)) void k_gn_rows_bwd(const typename
     Coeff k;
     k.mu = mean[blockIdx.x], k.r = rstd[blockIdx.x];
     typename P::R d[K], e[K];
-    each<V, MASK, K>(s, b, [&](int i, int, const Window& w) {
+    each<V, MASK, K>(s, b, [&](int i, int, const Window& w, bool) {
         d[i] = load<DT, V, MASK>(x, b, w);
         e[i] = load<DT, V, MASK>(dy, b, w);
     }, Nothing());
@@ -110,19 +115,21 @@ __global__ __launch_bounds__(threads_of(V, K)) void k_gn_rows_bwd(const typename
     const int lanes = 1 << s.lanes_log2, lane = int(threadIdx.x) & (lanes - 1);
     const int share = lanes > 64 ? lanes >> 6 : 1;
     float sa = 0.f, sb = 0.f;
-    each<V, MASK, K>(s, b, [&](int i, int row, const Window& w) {
+    each<V, MASK, K>(s, b, [&](int i, int row, const Window& w, bool on) {
         const float2 gb = row_params[row];
         k.ga = gb.x, k.be = gb.y;
-        float f[V], g[V];
+        float f[V], g[V], ta = 0.f, tb = 0.f;
         P::open(d[i], f);
         P::open(e[i], g);
 #pragma unroll
         for (int j = 0; j < V; ++j) {
             const float xh = normal(k, f[j]);
             const float du = in<MASK>(w, j) ? slope<ACT>(k, xh, g[j]) : 0.f;
-            sa += du;
-            sb = in<MASK>(w, j) ? fmaf(du, xh, sb) : sb;
+            ta += du;
+            tb = in<MASK>(w, j) ? fmaf(du, xh, tb) : tb;
         }
+        sa += on ? ta : 0.f;
+        sb += on ? tb : 0.f;
     }, [&](int row) {
         sa = run_sum(sa, lanes);
         sb = run_sum(sb, lanes);
@@ -146,7 +153,7 @@ __global__ __launch_bounds__(threads_of(V, K)) void k_gn_rows_bwd(const typename
     const float m = float(s.cg) * float(s.hw);
     const float2 both = block_sum2(s1, s2, part);
     s1 = both.x / m, s2 = both.y / m;
-    each<V, MASK, K>(s, b, [&](int i, int row, const Window& w) {
+    each<V, MASK, K>(s, b, [&](int i, int row, const Window& w, bool on) {
         const float2 gb = row_params[row];
         k.ga = gb.x, k.be = gb.y;
         float f[V], g[V];
@@ -154,7 +161,7 @@ __global__ __launch_bounds__(threads_of(V, K)) void k_gn_rows_bwd(const typename
         P::open(e[i], g);
 #pragma unroll
         for (int j = 0; j < V; ++j) f[j] = backward<ACT>(k, f[j], g[j], s1, s2);
-        store<DT, V, MASK>(dx, b, w, f);
+        if (on) store<DT, V, MASK>(dx, b, w, f);
     }, Nothing());
 }
 
@@ -173,14 +180,15 @@ __device__ __forceinline__ Piece piece_of(const Rows& s, int pieces) {
     p.c = int(p.row % unsigned(s.cg * s.groups));
     return p;
 }
-// Calls f(i, window): the windows of a row from `skip` vectors on.
+// Calls f(i, window, on): the vectors of a row from `skip` on, as above.
 template <int V, bool MASK, int K, class F>
 __device__ __forceinline__ void each_of_piece(const Rows& s, const Base<V, MASK>& b, int skip, F f) {
     const int lane = int(threadIdx.x & 63);
 #pragma unroll
     for (int i = 0; i < K; ++i) {
-        const Window w = window<V, MASK>(b, 0, s.hw, skip + i * 64 + lane);
-        if (w.hi > w.lo) f(i, w);
+        const int k = skip + i * 64 + lane;
+        const bool on = has<V, MASK>(b, 0, s.hw, k);
+        f(i, window<V, MASK>(b, 0, s.hw, on ? k : 0), on);
     }
 }
 
@@ -194,26 +202,28 @@ __global__ __launch_bounds__(256, 4) void k_gn_rowparts_fwd(const typename Elt<D
     const Base<V, MASK> b(s, int64_t(p.row) * s.hw);
     const int skip = p.piece * K * 64;
     typename P::R d[K];
-    each_of_piece<V, MASK, K>(s, b, skip, [&](int i, const Window& w) { d[i] = load<DT, V, MASK>(x, b, w); });
+    each_of_piece<V, MASK, K>(s, b, skip, [&](int i, const Window& w, bool) { d[i] = load<DT, V, MASK>(x, b, w); });
     float sum = 0.f, num = 0.f;
-    each_of_piece<V, MASK, K>(s, b, skip, [&](int i, const Window& w) {
-        float f[V];
+    each_of_piece<V, MASK, K>(s, b, skip, [&](int i, const Window& w, bool on) {
+        float f[V], t = 0.f;
         P::open(d[i], f);
-        num += float(w.hi - w.lo);
+        num += on ? float(w.hi - w.lo) : 0.f;
 #pragma unroll
-        for (int j = 0; j < V; ++j) sum += in<MASK>(w, j) ? f[j] : 0.f;
+        for (int j = 0; j < V; ++j) t += in<MASK>(w, j) ? f[j] : 0.f;
+        sum += on ? t : 0.f;
     });
     num = wave_sum(num);
     const float mu = num > 0.f ? wave_sum(sum) / num : 0.f;
     float sq = 0.f;
-    each_of_piece<V, MASK, K>(s, b, skip, [&](int i, const Window& w) {
-        float f[V];
+    each_of_piece<V, MASK, K>(s, b, skip, [&](int i, const Window& w, bool on) {
+        float f[V], t = 0.f;
         P::open(d[i], f);
 #pragma unroll
         for (int j = 0; j < V; ++j) {
             const float e = in<MASK>(w, j) ? f[j] - mu : 0.f;
-            sq = fmaf(e, e, sq);
+            t = fmaf(e, e, t);
         }
+        sq += on ? t : 0.f;
     });
     sq = wave_sum(sq);
     if ((threadIdx.x & 63) == 0) parts[p.id] = make_float4(mu, sq, num, 0.f);
@@ -234,14 +244,14 @@ __global__ __launch_bounds__(256, 4) void k_gn_rowwrite_fwd(const typename Elt<D
     const Base<V, MASK> b(s, int64_t(p.row) * s.hw);
     const int skip = p.piece * K * 64;
     typename P::R d[K];
-    each_of_piece<V, MASK, K>(s, b, skip, [&](int i, const Window& w) { d[i] = load<DT, V, MASK>(x, b, w); });
+    each_of_piece<V, MASK, K>(s, b, skip, [&](int i, const Window& w, bool) { d[i] = load<DT, V, MASK>(x, b, w); });
     const Coeff k = coeff_of(p, q, mean, rstd);
-    each_of_piece<V, MASK, K>(s, b, skip, [&](int i, const Window& w) {
+    each_of_piece<V, MASK, K>(s, b, skip, [&](int i, const Window& w, bool on) {
         float f[V];
         P::open(d[i], f);
 #pragma unroll
         for (int j = 0; j < V; ++j) f[j] = forward<ACT>(k, f[j]);
-        store<DT, V, MASK>(y, b, w, f);
+        if (on) store<DT, V, MASK>(y, b, w, f);
     });
 }
 
@@ -256,23 +266,25 @@ __global__ __launch_bounds__(256, 4) void k_gn_rowparts_bwd(const typename Elt<D
     const Base<V, MASK> b(s, int64_t(p.row) * s.hw);
     const int skip = p.piece * K * 64;
     typename P::R d[K], e[K];
-    each_of_piece<V, MASK, K>(s, b, skip, [&](int i, const Window& w) {
+    each_of_piece<V, MASK, K>(s, b, skip, [&](int i, const Window& w, bool) {
         d[i] = load<DT, V, MASK>(x, b, w);
         e[i] = load<DT, V, MASK>(dy, b, w);
     });
     const Coeff k = coeff_of(p, q, mean, rstd);
     float sa = 0.f, sb = 0.f;
-    each_of_piece<V, MASK, K>(s, b, skip, [&](int i, const Window& w) {
-        float f[V], g[V];
+    each_of_piece<V, MASK, K>(s, b, skip, [&](int i, const Window& w, bool on) {
+        float f[V], g[V], ta = 0.f, tb = 0.f;
         P::open(d[i], f);
         P::open(e[i], g);
 #pragma unroll
         for (int j = 0; j < V; ++j) {
             const float xh = normal(k, f[j]);
             const float du = in<MASK>(w, j) ? slope<ACT>(k, xh, g[j]) : 0.f;
-            sa += du;
-            sb = in<MASK>(w, j) ? fmaf(du, xh, sb) : sb;
+            ta += du;
+            tb = in<MASK>(w, j) ? fmaf(du, xh, tb) : tb;
         }
+        sa += on ? ta : 0.f;
+        sb += on ? tb : 0.f;
     });
     sa = wave_sum(sa);
     sb = wave_sum(sb);
@@ -291,19 +303,19 @@ __global__ __launch_bounds__(256, 4) void k_gn_rowwrite_bwd(const typename Elt<D
     const Base<V, MASK> b(s, int64_t(p.row) * s.hw);
     const int skip = p.piece * K * 64;
     typename P::R d[K], e[K];
-    each_of_piece<V, MASK, K>(s, b, skip, [&](int i, const Window& w) {
+    each_of_piece<V, MASK, K>(s, b, skip, [&](int i, const Window& w, bool) {
         d[i] = load<DT, V, MASK>(x, b, w);
         e[i] = load<DT, V, MASK>(dy, b, w);
     });
     const Coeff k = coeff_of(p, q, mean, rstd);
     const float2 sum = s12[p.ng];
-    each_of_piece<V, MASK, K>(s, b, skip, [&](int i, const Window& w) {
+    each_of_piece<V, MASK, K>(s, b, skip, [&](int i, const Window& w, bool on) {
         float f[V], g[V];
         P::open(d[i], f);
         P::open(e[i], g);
 #pragma unroll
         for (int j = 0; j < V; ++j) f[j] = backward<ACT>(k, f[j], g[j], sum.x, sum.y);
-        store<DT, V, MASK>(dx, b, w, f);
+        if (on) store<DT, V, MASK>(dx, b, w, f);
     });
 }
 
