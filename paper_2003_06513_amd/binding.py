@@ -179,9 +179,11 @@ def _dev(t, name):
 
 
 def _stream(stream):
+    """The handle of ``stream`` (None: the current one of the current device)."""
+    if stream is not None:
+        return stream.cuda_stream
     torch = _torch()
-    s = stream if stream is not None else torch.cuda.current_stream()
-    return s.cuda_stream
+    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
 
 
 def _torch_stream(stream):
@@ -621,12 +623,15 @@ class AdmmLayer:
 
 
 # ------------------------------------------------------------------ group normalisation
+def _current_device() -> int:
+    return _torch().cuda.current_device()
+
+
 def _same_device(*tensors):
     """The tensors of a call lie on the current device, whose streams it runs on."""
-    torch = _torch()
-    at = torch.cuda.current_device()
+    at = _current_device()
     for t in tensors:
-        if t is not None and t.device.index != at:
+        if t is not None and t.get_device() != at:
             raise ValueError("a tensor lies on %s, and the current device is cuda:%d" % (t.device, at))
 
 
@@ -642,24 +647,28 @@ def _layout(x) -> int:
 
 
 def _like(t, x, layout, name):
-    """The address of ``t``, which has the shape, type and layout of ``x``."""
+    """The address of ``t``, which has the shape, type, layout and device of ``x``."""
     torch = _torch()
-    if t.dtype != x.dtype or t.shape != x.shape or not t.is_cuda or not t.is_contiguous(
+    if t.dtype != x.dtype or t.shape != x.shape or t.get_device() != x.get_device() or not t.is_contiguous(
             memory_format=torch.channels_last if layout == PSC_NHWC else torch.contiguous_format):
-        raise ValueError("%s must have the shape, type and layout of x" % name)
-    return t.data_ptr() if t.numel() else None
+        raise ValueError("%s must have the shape, type, layout and device of x" % name)
+    return t.data_ptr() or None
 
 
-def _vector(t, numel, name):
-    if t is not None and t.numel() != numel:
-        raise ValueError("%s must have %d elements" % (name, numel))
-    return _f32(t, name)
+def _vector(t, numel, x, name):
+    """The address of the fp32 values ``t`` (may be None) on the device of ``x``."""
+    if t is None:
+        return None
+    if t.dtype != _torch().float32 or t.numel() != numel or t.get_device() != x.get_device() or not t.is_contiguous():
+        raise ValueError("%s must have %d contiguous float32 elements on the device of x" % (name, numel))
+    return t.data_ptr() or None
 
 
 def _act_code(act) -> int:
-    if act not in ACTIVATIONS:
+    code = ACTIVATIONS.get(act)
+    if code is None:
         raise ValueError("act must be one of %s" % ", ".join(ACTIVATIONS))
-    return ACTIVATIONS[act]
+    return code
 
 
 def group_norm_workspace(dtype: int, layout: int, n: int, c: int, h: int, w: int, groups: int,
@@ -671,12 +680,26 @@ def group_norm_workspace(dtype: int, layout: int, n: int, c: int, h: int, w: int
     return int(b.value)
 
 
-def _norm_scratch(ws, args, backward, stream):
-    """The address and size of ``ws``, or of scratch of this call's own."""
+_NORM_SCRATCH: dict = {}    # group_norm_workspace by its arguments, at most 4096 of them
+
+
+def _norm_scratch(ws, stream, *args):
+    """The address and size of ``ws``, or of scratch of this call's own (its
+    size kept by the sizes of the call alone), and the tensor."""
     if ws is None:
-        need = group_norm_workspace(*args, backward)
-        ws = _scratch(need, stream) if need else None
-    return ws, _dev(ws, "ws"), _ws_bytes(ws)
+        need = _NORM_SCRATCH.get(args)
+        if need is None:
+            need = group_norm_workspace(*args)
+            if len(_NORM_SCRATCH) >= 4096:
+                _NORM_SCRATCH.clear()
+            _NORM_SCRATCH[args] = need
+        if need:
+            ws = _scratch(need, stream)
+        if ws is None:
+            return None, 0, None
+    else:
+        _same_device(ws)
+    return _dev(ws, "ws"), _ws_bytes(ws), ws
 
 
 def group_norm_fwd(x, groups: int, gamma, beta, y, eps: float = 1e-5, act: str = "none", mean=None, rstd=None,
@@ -685,15 +708,15 @@ def group_norm_fwd(x, groups: int, gamma, beta, y, eps: float = 1e-5, act: str =
     of channels of x [n, c, h, w], contiguous or channels_last (y the same);
     gamma and beta (fp32, or None), and mean and rstd (fp32 [n, groups], or
     None), which group_norm_bwd reads.  act: "none", "relu" or "silu"."""
-    layout, code, dt = _layout(x), _act_code(act), dtype_code(x)
+    layout, dt = _layout(x), dtype_code(x)
     n, c, h, w = x.shape
     groups = int(groups)
-    _same_device(x, gamma, beta, y, mean, rstd, ws)
-    keep, wp, wb = _norm_scratch(ws, (dt, layout, n, c, h, w, groups), False, stream)
-    _check(lib().psc_group_norm_fwd(dt, layout, x.data_ptr() if n else None, n, c, h, w, groups,
-                                    _vector(gamma, c, "gamma"), _vector(beta, c, "beta"), float(eps), code,
-                                    _like(y, x, layout, "y"), _vector(mean, n * groups, "mean"),
-                                    _vector(rstd, n * groups, "rstd"), wp, wb, _stream(stream)), "psc_group_norm_fwd")
+    _same_device(x)
+    wp, wb, ws = _norm_scratch(ws, stream, dt, layout, n, c, h, w, groups, False)
+    _check(lib().psc_group_norm_fwd(dt, layout, x.data_ptr() or None, n, c, h, w, groups, _vector(gamma, c, x, "gamma"),
+                                    _vector(beta, c, x, "beta"), eps, _act_code(act), _like(y, x, layout, "y"),
+                                    _vector(mean, n * groups, x, "mean"), _vector(rstd, n * groups, x, "rstd"), wp, wb,
+                                    _stream(stream)), "psc_group_norm_fwd")
 
 
 def group_norm_bwd(x, dy, groups: int, gamma, beta, mean, rstd, dx, dgamma=None, dbeta=None, act: str = "none",
@@ -701,16 +724,16 @@ def group_norm_bwd(x, dy, groups: int, gamma, beta, mean, rstd, dx, dgamma=None,
     """psc_group_norm_bwd: dx, and dgamma and dbeta (fp32 [c], or None), from
     the gradient dy of group_norm_fwd's output and the statistics that it
     wrote; dy and dx have the type and layout of x."""
-    layout, code, dt = _layout(x), _act_code(act), dtype_code(x)
+    layout, dt = _layout(x), dtype_code(x)
     n, c, h, w = x.shape
     groups = int(groups)
-    _same_device(x, dy, gamma, beta, mean, rstd, dx, dgamma, dbeta, ws)
-    keep, wp, wb = _norm_scratch(ws, (dt, layout, n, c, h, w, groups), True, stream)
-    _check(lib().psc_group_norm_bwd(dt, layout, x.data_ptr() if n else None, _like(dy, x, layout, "dy"), n, c, h, w,
-                                    groups, _vector(gamma, c, "gamma"), _vector(beta, c, "beta"),
-                                    _vector(mean, n * groups, "mean"), _vector(rstd, n * groups, "rstd"), code,
-                                    _like(dx, x, layout, "dx"), _vector(dgamma, c, "dgamma"),
-                                    _vector(dbeta, c, "dbeta"), wp, wb, _stream(stream)), "psc_group_norm_bwd")
+    _same_device(x)
+    wp, wb, ws = _norm_scratch(ws, stream, dt, layout, n, c, h, w, groups, True)
+    _check(lib().psc_group_norm_bwd(dt, layout, x.data_ptr() or None, _like(dy, x, layout, "dy"), n, c, h, w, groups,
+                                    _vector(gamma, c, x, "gamma"), _vector(beta, c, x, "beta"),
+                                    _vector(mean, n * groups, x, "mean"), _vector(rstd, n * groups, x, "rstd"),
+                                    _act_code(act), _like(dx, x, layout, "dx"), _vector(dgamma, c, x, "dgamma"),
+                                    _vector(dbeta, c, x, "dbeta"), wp, wb, _stream(stream)), "psc_group_norm_bwd")
 
 
 # ------------------------------------------------------------------ the optimiser
@@ -730,8 +753,7 @@ class ParamList:
         torch = _torch()
         grads = list(grads)
         k = len(grads)
-        params, m, v, scale, copies = (list(t) if t is not None else [None] * k
-                                       for t in (params, m, v, scale, copies))
+        params, m, v, scale, copies = (list(t) if t is not None else [None] * k for t in (params, m, v, scale, copies))
         decay = list(weight_decay) if hasattr(weight_decay, "__len__") else [weight_decay] * k
         if not all(len(t) == k for t in (params, m, v, scale, copies, decay)):
             raise ValueError("every list must have one entry for each gradient")

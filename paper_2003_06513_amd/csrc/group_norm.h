@@ -64,8 +64,9 @@ template <int ACT> __device__ __forceinline__ float backward(const Coeff& k, flo
 }
 
 typedef uint32_t u4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u2 __attribute__((ext_vector_type(2)));
 
-// V elements as they lie in memory: 16 bytes, or one element.
+// V elements as they lie in memory: 16 bytes, 8, or one element.
 template <int DT, int V> struct Pack;
 template <> struct Pack<DT_F32, 4> {
     using R = u4;
@@ -101,6 +102,24 @@ template <> struct Pack<DT_F16, 8> {
         return r;
     }
 };
+template <> struct Pack<DT_F16, 4> {
+    using R = u2;
+    __device__ __forceinline__ static void open(const R& r, float (&f)[4]) {
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const uint32_t b = r[j];
+            f[2 * j] = float(__builtin_bit_cast(_Float16, uint16_t(b)));
+            f[2 * j + 1] = float(__builtin_bit_cast(_Float16, uint16_t(b >> 16)));
+        }
+    }
+    __device__ __forceinline__ static R close(const float (&f)[4]) {
+        R r;
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+            r[j] = uint32_t(Elt<DT_F16>::from_f(f[2 * j])) | uint32_t(Elt<DT_F16>::from_f(f[2 * j + 1])) << 16;
+        return r;
+    }
+};
 template <int DT> struct Pack<DT, 1> {
     using R = typename Elt<DT>::T;
     __device__ __forceinline__ static void open(const R& r, float (&f)[1]) { f[0] = Elt<DT>::load(&r, 0); }
@@ -124,6 +143,10 @@ template <int OFF> __device__ __forceinline__ float lane_step(float x) {
         constexpr int ctrl = OFF == 1 ? 0xB1 : OFF == 2 ? 0x4E : OFF == 4 ? 0x141 : 0x140;
         return x + __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, b, ctrl, 0xf, 0xf, true));
     }
+}
+// x plus the x of the lane BY further on in its row of 16.
+template <int BY> __device__ __forceinline__ float turned_sum(float x) {
+    return x + __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), 0x120 + BY, 0xf, 0xf, true));
 }
 __device__ __forceinline__ float wave_sum(float x) {
     x = lane_step<1>(x), x = lane_step<2>(x), x = lane_step<4>(x), x = lane_step<8>(x);
@@ -171,6 +194,77 @@ template <class R, class T> __device__ __forceinline__ R get(const T* base, uint
 }
 template <class R, class T> __device__ __forceinline__ void put(T* base, uint32_t byte, const R& r) {
     *reinterpret_cast<R*>(reinterpret_cast<char*>(base) + byte) = r;
+}
+
+// Where the sums of channels go: [n][c][pieces], and, where an image is the
+// whole batch, the parameters' gradients at once.
+struct Sums {
+    float2* ab;
+    float* dgamma;
+    float* dbeta;
+};
+// dbeta and dgamma from the sums: the blocks from `first` on of a launch add 8
+// channels each, over the images and pieces, blockDim / 8 of them at a time,
+// in a fixed order.
+struct Tail {
+    const float2* sums;
+    int n, c, pieces;
+    float* dgamma;
+    float* dbeta;
+    unsigned first;
+};
+__device__ __forceinline__ void param_block(const Tail& t) {
+    __shared__ float2 part[16][8];
+    const int k = int(blockIdx.x - t.first) * 8 + int(threadIdx.x & 7);
+    float a = 0.f, b = 0.f;
+    if (k < t.c) {
+        const unsigned count = unsigned(t.n) * unsigned(t.pieces);
+        for (unsigned i = threadIdx.x >> 3; i < count; i += blockDim.x >> 3) {
+            const unsigned img = i / unsigned(t.pieces), piece = i - img * unsigned(t.pieces);
+            const float2 ab = t.sums[(int64_t(img) * t.c + k) * t.pieces + piece];
+            a += ab.x;
+            b += ab.y;
+        }
+    }
+    a = turned_sum<8>(a), b = turned_sum<8>(b);
+    a = lane_step<32>(lane_step<16>(a)), b = lane_step<32>(lane_step<16>(b));
+    if ((threadIdx.x & 63) < 8) part[threadIdx.x >> 6][threadIdx.x & 7] = make_float2(a, b);
+    __syncthreads();
+    if (threadIdx.x < 8 && k < t.c) {
+        a = 0.f, b = 0.f;
+        for (unsigned i = 0; i < blockDim.x >> 6; ++i) a += part[i][threadIdx.x].x, b += part[i][threadIdx.x].y;
+        if (t.dgamma) t.dgamma[k] = b;
+        if (t.dbeta) t.dbeta[k] = a;
+    }
+}
+
+// The statistics of a group from its pieces, by a run of `lanes` lanes: the
+// means weighted by their counts, the squares about the common mean.
+__device__ __forceinline__ float2 joined_stats(const float4* p, int count, int lane, int lanes, float eps) {
+    float sum = 0.f, num = 0.f;
+    for (int i = lane; i < count; i += lanes) {
+        sum = fmaf(p[i].z, p[i].x, sum);
+        num += p[i].z;
+    }
+    num = run_sum(num, lanes);
+    const float mu = run_sum(sum, lanes) / num;
+    float sq = 0.f;
+    for (int i = lane; i < count; i += lanes) {
+        const float d = p[i].x - mu;
+        sq += fmaf(p[i].z * d, d, p[i].y);
+    }
+    return make_float2(mu, 1.f / sqrtf(run_sum(sq, lanes) / num + eps));
+}
+// S1 / M and S2 / M of the group whose channels begin with gamma[0].
+__device__ __forceinline__ float2 joined_back(const float2* p, int count, int pieces, const float* gamma, float m, int lane,
+                                              int lanes) {
+    float s1 = 0.f, s2 = 0.f;
+    for (int i = lane; i < count; i += lanes) {
+        const float ga = or_one(gamma, i / pieces);
+        s1 = fmaf(ga, p[i].x, s1);
+        s2 = fmaf(ga, p[i].y, s2);
+    }
+    return make_float2(run_sum(s1, lanes) / m, run_sum(s2, lanes) / m);
 }
 
 // ---- NCHW.  A channel of an image is a row of hw elements; rows lie one
@@ -280,10 +374,12 @@ struct Cols {
     int hw;
     int tile;           // channels of a block
     int tiles;
+    int near;           // tiles that share lines of memory
     int cols_log2;
     int pixels;         // pixels of a block
     int chunks;         // blocks that share the pixels of an image
     uint32_t cg_m;      // 2^32 / cg, rounded up
+    int join_lanes;     // lanes that join a group's pieces
 };
 // k / cg for k, cg < 2^16 (cg_m is at most cg - 1 too large: less than 2^32 / cg in the product); cg == 1: 0.
 __device__ __forceinline__ int group_of(const Cols& q, int k) { return q.cg_m ? int(__umulhi(uint32_t(k), q.cg_m)) : k; }
@@ -296,17 +392,16 @@ __device__ __forceinline__ int sum_rows(const Cols& q) { return int(blockDim.x >
 template <int V>
 __device__ __forceinline__ void wave_channels(float (&s)[V], const Cols& q, int width, float* buf) {
     const int cols = 1 << q.cols_log2, col = int(threadIdx.x) & (cols - 1);
-    // lanes that differ in the bits from `cols` on have the same channels; the mirrors within 16 lanes want the
-    // smaller bits summed before, so those steps go by exchange
-    for (int off = cols; off < 16; off <<= 1)
+    // the lanes of a row of 16 by turning it, which keeps the columns below the turn apart
 #pragma unroll
-        for (int j = 0; j < V; ++j) s[j] += __shfl_xor(s[j], off);
-    if (cols <= 16)
-#pragma unroll
-        for (int j = 0; j < V; ++j) s[j] = lane_step<16>(s[j]);
-    if (cols <= 32)
-#pragma unroll
-        for (int j = 0; j < V; ++j) s[j] = lane_step<32>(s[j]);
+    for (int j = 0; j < V; ++j) {
+        if (cols <= 8) s[j] = turned_sum<8>(s[j]);
+        if (cols <= 4) s[j] = turned_sum<4>(s[j]);
+        if (cols <= 2) s[j] = turned_sum<2>(s[j]);
+        if (cols <= 1) s[j] = turned_sum<1>(s[j]);
+        if (cols <= 16) s[j] = lane_step<16>(s[j]);
+        if (cols <= 32) s[j] = lane_step<32>(s[j]);
+    }
     if (int(threadIdx.x & 63u) < cols && col * V < width) {
         float* to = buf + int(threadIdx.x >> span_log2(q)) * q.tile + col * V;
 #pragma unroll
@@ -329,6 +424,7 @@ struct Params {
 // How a call runs (host).  pieces: partial sums of each channel, [n][c][pieces].
 struct Plan {
     bool held;          // a block holds its whole groups
+    bool joined;        // else: who writes a piece adds up its group's pieces itself
     int vec;            // 0: single elements, 1: 16 bytes, 2: 16 bytes with windows
     int k;              // vectors per thread, rounded up to a compiled count
     int threads;
@@ -337,13 +433,19 @@ struct Plan {
     Rows rows;
     Cols cols;
 };
-// Vectors per lane of the kernels that work piece by piece: 16 bytes, single elements.
-constexpr int kPiece = 8, kPieceSingle = 32;
-// Threads of the kernels that hold their groups: the registers of K vectors for
-// so many (kept below 128 of 1024 threads, 256 of 512).
-constexpr int threads_of(int v, int k) { return k <= 4 || (v == 1 && k <= 8) ? 1024 : 512; }
-// The most vectors per thread of the kernels that hold their groups.
-constexpr int kMostFwd = 16, kMostBwd = 8, kMostSingle = 32;
+// Elements of a vector.  The backward with the channels last holds six values
+// for each channel of a thread besides x and dy: with eight channels of fp16
+// it took more than 128 registers and one block filled a CU (512 @ 28x28 b64:
+// 62 us), so it takes four.
+constexpr int vector_of(int dtype, bool columns_back) { return dtype == DT_F16 && !columns_back ? 8 : 4; }
+// Vectors per lane of the kernels that work piece by piece: 128 bytes, or as
+// many single elements.
+constexpr int kPieceSingle = 16;
+constexpr int piece_of(int dtype, int v) { return v == 1 ? kPieceSingle : 128 / (v * (dtype == DT_F16 ? 2 : 4)); }
+// The most vectors per thread of the kernels that hold their groups, and the
+// threads that leave registers for so many.
+constexpr int most_of(int dtype, int v, bool back) { return v == 1 ? 32 : (back ? 1 : 2) * piece_of(dtype, v); }
+constexpr int threads_of(int dtype, int v, int k) { return 2 * k <= piece_of(dtype, v) ? 1024 : 512; }
 
 // Calls go with the compiled activation and count of vectors per thread.
 template <class F> void with_act(int act, F go) {
@@ -351,15 +453,16 @@ template <class F> void with_act(int act, F go) {
     else if (act == ACT_RELU) go(IntC<ACT_RELU>{});
     else go(IntC<ACT_SILU>{});
 }
-template <int V, bool BACK, class F> void with_count(int k, F go) {
+template <int DT, int V, bool BACK, class F> void with_count(int k, F go) {
     if constexpr (V == 1) {
         if (k <= 8) go(IntC<8>{});
-        else go(IntC<kMostSingle>{});
+        else go(IntC<32>{});
     } else {
-        if (k <= 2) go(IntC<2>{});
-        else if (k <= 4) go(IntC<4>{});
-        else if (k <= 8) go(IntC<8>{});
-        else if constexpr (!BACK) go(IntC<kMostFwd>{});
+        constexpr int n = piece_of(DT, V);
+        if (k <= n / 4) go(IntC<n / 4>{});
+        else if (k <= n / 2) go(IntC<n / 2>{});
+        else if (k <= n) go(IntC<n>{});
+        else if constexpr (!BACK) go(IntC<2 * n>{});
     }
 }
 
@@ -371,11 +474,14 @@ inline unsigned cols_lds(const Cols& q, int threads, int sums, int more) {
 template <int DT> void rows_fwd(const Plan& p, int64_t count, const void* x, const Params& q, float eps, void* y,
                                 float* mean, float* rstd, float4* parts, hipStream_t st);
 template <int DT> void rows_bwd(const Plan& p, int64_t count, const void* x, const void* dy, const Params& q,
-                                const float* mean, const float* rstd, void* dx, float2* parts, float2* s12, hipStream_t st);
+                                const float* mean, const float* rstd, void* dx, const Sums& sums, float2* s12,
+                                Tail tail, hipStream_t st);
 template <int DT> void cols_fwd(const Plan& p, int n, const void* x, const Params& q, float eps, void* y, float* mean,
                                 float* rstd, float4* parts, hipStream_t st);
 template <int DT> void cols_bwd(const Plan& p, int n, const void* x, const void* dy, const Params& q, const float* mean,
-                                const float* rstd, void* dx, float2* parts, float2* s12, hipStream_t st);
+                                const float* rstd, void* dx, const Sums& sums, float2* s12, Tail tail, hipStream_t st);
+// The blocks that a tail adds to a launch.
+inline unsigned tail_blocks(const Tail& t) { return t.dgamma || t.dbeta ? unsigned(t.c + 7) / 8u : 0u; }
 // Between the two passes over pieces (group_norm.hip): the statistics of each
 // of `groups` groups, or S1 / M and S2 / M, from its parts.
 void combine_fwd(const float4* parts, int64_t groups, int per_group, float eps, float* mean, float* rstd, hipStream_t st);

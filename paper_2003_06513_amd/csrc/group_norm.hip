@@ -1,17 +1,15 @@
 // Group normalisation: how a call runs, and the sums between the passes over
 // pieces.
-#include <cstdlib>
 #include "group_norm.h"
 
 namespace psc {
 namespace gn {
 namespace {
 
-// The statistics of a group from its pieces: the means weighted by their
-// counts, the squares about the common mean.
+// A block per group of many pieces.
 __global__ __launch_bounds__(256) void k_gn_combine_fwd(const float4* __restrict__ parts, int per, float eps,
                                                         float* __restrict__ mean, float* __restrict__ rstd) {
-    __shared__ float part[32];
+    __shared__ float part[32], again[16];
     const float4* p = parts + int64_t(blockIdx.x) * per;
     float sum = 0.f, num = 0.f;
     for (int i = threadIdx.x; i < per; i += 256) {
@@ -19,18 +17,16 @@ __global__ __launch_bounds__(256) void k_gn_combine_fwd(const float4* __restrict
         num += p[i].z;
     }
     const float2 both = block_sum2(num, sum, part);
-    num = both.x;
-    const float mu = both.y / num;
+    const float mu = both.y / both.x;
     float sq = 0.f;
     for (int i = threadIdx.x; i < per; i += 256) {
         const float d = p[i].x - mu;
         sq += fmaf(p[i].z * d, d, p[i].y);
     }
-    __syncthreads();
-    sq = block_sum(sq, part);
+    sq = block_sum(sq, again);
     if (threadIdx.x == 0) {
         mean[blockIdx.x] = mu;
-        rstd[blockIdx.x] = 1.f / sqrtf(sq / num + eps);
+        rstd[blockIdx.x] = 1.f / sqrtf(sq / both.x + eps);
     }
 }
 
@@ -50,31 +46,7 @@ __global__ __launch_bounds__(256) void k_gn_combine_bwd(const float2* __restrict
     if (threadIdx.x == 0) s12[blockIdx.x] = make_float2(sum.x / m, sum.y / m);
 }
 
-// dbeta and dgamma: a block adds 32 channels, each over the images' and
-// pieces' sums, 32 of them at a time, in a fixed order.
-__global__ __launch_bounds__(1024) void k_gn_param(const float2* __restrict__ sums, int n, int c, int pieces,
-                                                   float* __restrict__ dgamma, float* __restrict__ dbeta) {
-    __shared__ float2 part[32][33];
-    const int k = int(blockIdx.x) * 32 + int(threadIdx.x & 31), row = int(threadIdx.x >> 5);
-    float a = 0.f, b = 0.f;
-    if (k < c) {
-        const int64_t count = int64_t(n) * pieces;
-        for (int64_t i = row; i < count; i += 32) {
-            const int64_t img = i / pieces, piece = i - img * pieces;
-            const float2 ab = sums[(img * c + k) * pieces + piece];
-            a += ab.x;
-            b += ab.y;
-        }
-    }
-    part[row][threadIdx.x & 31] = make_float2(a, b);
-    __syncthreads();
-    if (row == 0 && k < c) {
-        a = 0.f, b = 0.f;
-        for (int i = 0; i < 32; ++i) a += part[i][threadIdx.x].x, b += part[i][threadIdx.x].y;
-        if (dgamma) dgamma[k] = b;
-        if (dbeta) dbeta[k] = a;
-    }
-}
+__global__ __launch_bounds__(1024) void k_gn_param(Tail t) { param_block(t); }
 
 int log2_ceil(int64_t x) {
     int l = 0;
@@ -83,16 +55,26 @@ int log2_ceil(int64_t x) {
 }
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
-int vector_of(int dtype) { return dtype == DT_F16 ? 8 : 4; }
-
+// Blocks by size, for units of work that there are many of (small blocks,
+// a few vectors a thread) or few of (every thread one or two): threads, and
+// the most sixteenths of the bytes that a thread can hold of one tensor.
 struct Try {
-    int threads, k;
+    int threads, part;
 };
-// Blocks by size, for units of work that there are many of (a few vectors a
-// thread, small blocks) or few of (every thread one or two).
-constexpr Try kMany[] = {{64, 4}, {128, 4}, {256, 4}, {256, 8}, {512, 8}, {1024, 4}, {512, 32}};
-constexpr Try kFew[] = {{64, 2}, {128, 2}, {256, 2}, {512, 2}, {1024, 2}, {1024, 4}, {512, 8}, {512, 32}};
-int most_of(bool backward, int vec) { return vec == 0 ? kMostSingle : backward ? kMostBwd : kMostFwd; }
+constexpr Try kMany[] = {{64, 8}, {128, 8}, {256, 8}, {256, 16}, {512, 16}, {1024, 8}, {512, 32}};
+constexpr Try kFew[] = {{64, 4}, {128, 4}, {256, 4}, {512, 4}, {1024, 4}, {1024, 8}, {512, 16}, {512, 32}};
+// The first of them that `count(threads)` vectors a thread fit, or none.
+template <class F> bool choose(int64_t units, int dtype, int v, bool backward, Plan& p, F count) {
+    const Try* list = units >= 512 ? kMany : kFew;
+    const int n = units >= 512 ? int(sizeof(kMany) / sizeof(Try)) : int(sizeof(kFew) / sizeof(Try));
+    for (int i = 0; i < n; ++i) {
+        const int64_t k = count(list[i].threads);
+        if (k < 1 || k > most_of(dtype, v, backward) || 16 * k > int64_t(list[i].part) * piece_of(dtype, v)) continue;
+        p.held = true, p.threads = list[i].threads, p.k = int(k), p.pieces = 1;
+        return true;
+    }
+    return false;
+}
 
 // The lanes that share a row so that a thread has the fewest vectors.
 int64_t rows_slots(int cg, int vpr, int threads, int* lanes_log2, int* vi) {
@@ -104,91 +86,87 @@ int64_t rows_slots(int cg, int vpr, int threads, int* lanes_log2, int* vi) {
     return best;
 }
 
+// The most sums of pieces that every wave that writes one reads itself, and
+// every block of columns.  More of them are joined by a launch of its own
+// (about 2.5 us).
+constexpr int kJoined = 256, kJoinedCols = 2048;
+
 // The plan of a call whose tensors allow 16-byte accesses (vec 1: at the
 // beginning of each row, 2: within rows) or not (0).
 Plan plan_rows(const GroupNormArgs& a, bool backward, int vec) {
     Plan p{};
-    const int v = vec ? vector_of(a.dtype) : 1;
+    const int v = vec ? vector_of(a.dtype, false) : 1;
     Rows& s = p.rows;
     s.cg = a.c / a.groups, s.groups = a.groups, s.hw = a.h * a.w;
     s.total = int64_t(a.n) * a.c * s.hw;
     s.vpr = vec == 2 ? int(ceil_div(s.hw + v - 1, v)) : int(ceil_div(s.hw, v));
     p.vec = vec;
-    const int64_t units = int64_t(a.n) * a.groups;
-    const auto fits = [&](const Try& t) {
-        const int64_t n = rows_slots(s.cg, s.vpr, t.threads, &s.lanes_log2, &s.vi);
-        if (n > t.k || n > most_of(backward, vec)) return false;
-        p.held = true, p.threads = t.threads, p.k = s.slots = int(n), p.grid = units, p.pieces = 1;
-        return true;
-    };
-    if (vec && s.cg <= 2048) {      // the rows' parameters and sums fit the LDS
-        if (units >= 512) {
-            for (const Try& t : kMany)
-                if (fits(t)) return p;
-        } else {
-            for (const Try& t : kFew)
-                if (fits(t)) return p;
-        }
+    p.grid = int64_t(a.n) * a.groups;
+    if (vec && s.cg <= 2048 &&      // the rows' parameters and sums fit the LDS
+        choose(p.grid, a.dtype, v, backward, p, [&](int threads) {
+            return rows_slots(s.cg, s.vpr, threads, &s.lanes_log2, &s.vi);
+        })) {
+        s.slots = p.k;
+        return p;
     }
-    p.pieces = int(ceil_div(s.vpr, 64 * (vec ? kPiece : kPieceSingle)));
+    p.pieces = int(ceil_div(s.vpr, 64 * piece_of(a.dtype, v)));
+    p.joined = int64_t(s.cg) * p.pieces <= kJoined;
     return p;
 }
 
+// Blocks of the columns, in slabs of tiles that share lines of memory.
+int64_t cols_grid(Cols& s, int n, int elt) {
+    s.near = 128 / (s.tile * elt);
+    if (s.near < 1) s.near = 1;
+    if (s.near > s.tiles || int64_t(n) * s.chunks >= 64) s.near = s.tiles;
+    return ceil_div(int64_t(n) * s.chunks * ceil_div(s.tiles, s.near), 8) * 8 * s.near;
+}
+
 Plan plan_cols(const GroupNormArgs& a, bool backward, int vec) {
-    Plan p{};
-    const int v = vec ? vector_of(a.dtype) : 1, elt = a.dtype == DT_F16 ? 2 : 4;
+    const int v = vec ? vector_of(a.dtype, backward) : 1, elt = a.dtype == DT_F16 ? 2 : 4;
+    Plan p{}, best{};
     Cols& s = p.cols;
-    s.c = a.c, s.groups = a.groups, s.cg = a.c / a.groups, s.hw = a.h * a.w;
     p.vec = vec;
+    s.c = a.c, s.groups = a.groups, s.cg = a.c / a.groups, s.hw = a.h * a.w;
     s.cg_m = s.cg == 1 ? 0 : uint32_t(((uint64_t(1) << 32) + s.cg - 1) / s.cg);
     int unit = s.cg;        // the fewest channels that are whole groups and whole vectors
     while (unit % v) unit += s.cg;
-    // Tiles as wide as a cache line, or half or a quarter of one, of whole groups.
-    const int want = getenv("GN_UNITS") ? atoi(getenv("GN_UNITS")) : 512;
-    const int least = getenv("GN_LEAST") ? atoi(getenv("GN_LEAST")) : 16;
-    Plan best{};
-    for (int bytes = 128; bytes >= least; bytes /= 2) {
+    // Tiles of whole groups, a line of memory wide or a part of one: as wide as gives every CU a block.
+    for (int bytes = 128; bytes >= 16; bytes /= 2) {
         const int tile = int(ceil_div(bytes, int64_t(unit) * elt)) * unit;
         s.tile = tile < a.c ? tile : a.c;
         s.tiles = int(ceil_div(a.c, s.tile));
         s.cols_log2 = log2_ceil(ceil_div(s.tile, v));
+        if (int64_t(s.hw) * a.c * elt >> 32) break;     // offsets of 32 bits
         const int64_t units = int64_t(a.n) * s.tiles;
-        const auto fits = [&](const Try& t) {
-            if (t.threads < (1 << s.cols_log2) || int64_t(s.hw) * a.c * elt >> 32) return false;
-            const int64_t n = ceil_div(s.hw, t.threads >> s.cols_log2);
-            if (n > t.k || n > most_of(backward, vec)) return false;
-            if (cols_lds(s, t.threads, backward ? 2 : 1, backward ? 4 : 2) > 60 * 1024) return false;
-            p.held = true, p.threads = t.threads, p.k = int(n), p.pieces = 1;
+        p.held = false;
+        if (choose(units, a.dtype, v, backward, p, [&](int threads) {
+                if (threads < (1 << s.cols_log2) ||
+                    cols_lds(s, threads, backward ? 2 : 1, backward ? 4 : 2) > 60 * 1024)
+                    return int64_t(0);
+                return ceil_div(s.hw, threads >> s.cols_log2);
+            })) {
             s.pixels = s.hw, s.chunks = 1;
-            p.grid = ceil_div(a.n, 8) * 8 * s.tiles;
-            return true;
-        };
-        bool found = false;
-        if (units >= 512) {
-            for (const Try& t : kMany)
-                if (!found) found = fits(t);
-        } else {
-            for (const Try& t : kFew)
-                if (!found) found = fits(t);
+            p.grid = cols_grid(s, a.n, elt);
+            best = p;
+            if (units >= 256) break;
         }
-        if (found) best = p;
-        if (found && units >= want) break;
     }
-    if (best.held && !getenv("GN_PIECES")) return best;
-    p = best = Plan{};
-    p.vec = vec;
-    s.c = a.c, s.groups = a.groups, s.cg = a.c / a.groups, s.hw = a.h * a.w;
-    s.cg_m = s.cg == 1 ? 0 : uint32_t(((uint64_t(1) << 32) + s.cg - 1) / s.cg);
-    // pieces: 256 threads, up to 16 vectors (64 single channels) side by side
-    s.cols_log2 = log2_ceil(ceil_div(a.c, v));
-    const int most = vec ? 4 : 6;
-    if (s.cols_log2 > most) s.cols_log2 = most;
-    s.tile = v << s.cols_log2;
+    if (best.held) return best;
+    // Pieces: 256 threads, whole groups if 16 vectors (64 single channels) side by side have room for one.
+    p.held = false;
+    const int room = vec ? 16 * v : 64;
+    s.tile = unit <= room ? room / unit * unit : room;
+    if (s.tile > a.c) s.tile = int(ceil_div(a.c, v)) * v;
+    s.cols_log2 = log2_ceil(ceil_div(s.tile, v));
     s.tiles = int(ceil_div(a.c, s.tile));
-    s.pixels = (256 >> s.cols_log2) * (vec ? kPiece : kPieceSingle);
+    s.pixels = (256 >> s.cols_log2) * piece_of(a.dtype, v);
     s.chunks = p.pieces = int(ceil_div(s.hw, s.pixels));
     p.threads = 256;
-    p.grid = ceil_div(a.n, 8) * 8 * s.tiles * s.chunks;
+    p.grid = cols_grid(s, a.n, elt);
+    p.joined = unit <= room && int64_t(s.tile) * s.chunks <= kJoinedCols;
+    s.join_lanes = 64;
+    while (s.join_lanes > 4 && s.join_lanes * (s.tile / s.cg) > 256) s.join_lanes /= 2;
     return p;
 }
 
@@ -196,13 +174,15 @@ Plan plan_of(const GroupNormArgs& a, bool backward, int vec) {
     return a.channels_last ? plan_cols(a, backward, vec) : plan_rows(a, backward, vec);
 }
 
-// How the tensors lie: all alike to 16 bytes, and rows (pixels) of whole vectors.
-int vec_of(const GroupNormArgs& a, const void* x, const void* y, const void* z) {
-    const uintptr_t at = reinterpret_cast<uintptr_t>(x) & 15u;
+// How the tensors lie: all alike to the bytes of a vector, and rows (pixels) of whole vectors.
+int vec_of(const GroupNormArgs& a, bool backward, const void* x, const void* y, const void* z) {
+    const bool columns_back = a.channels_last && backward;
+    const int v = vector_of(a.dtype, columns_back);
+    const uintptr_t mask = uintptr_t(v) * (a.dtype == DT_F16 ? 2 : 4) - 1, at = reinterpret_cast<uintptr_t>(x) & mask;
     for (const void* p : {y, z})
-        if (p && (reinterpret_cast<uintptr_t>(p) & 15u) != at) return 0;
+        if (p && (reinterpret_cast<uintptr_t>(p) & mask) != at) return 0;
     const int64_t row = a.channels_last ? a.c : int64_t(a.h) * a.w;
-    if (at == 0 && row % vector_of(a.dtype) == 0) return 1;
+    if (at == 0 && row % v == 0) return 1;
     return a.channels_last ? 0 : 2;
 }
 
@@ -239,11 +219,11 @@ size_t group_norm_workspace_bytes(const GroupNormArgs& a, bool backward) {
 hipError_t launch_group_norm_fwd(const GroupNormArgs& a, const void* x, const float* gamma, const float* beta, float eps,
                                  void* y, float* mean, float* rstd, void* ws, hipStream_t stream) {
     using namespace gn;
-    Plan p = plan_of(a, false, vec_of(a, x, y, nullptr));
+    Plan p = plan_of(a, false, vec_of(a, false, x, y, nullptr));
     const Params q{gamma, beta, a.act};
     float4* parts = static_cast<float4*>(ws);
     const int64_t rows = int64_t(a.n) * a.c * p.pieces, groups = int64_t(a.n) * a.groups;
-    if (!p.held && !mean) {
+    if (!p.held && !p.joined && !mean) {
         mean = static_cast<float*>(static_cast<void*>(parts + rows));
         rstd = mean + groups;
     }
@@ -262,26 +242,30 @@ hipError_t launch_group_norm_bwd(const GroupNormArgs& a, const void* x, const vo
                                  const float* beta, const float* mean, const float* rstd, void* dx, float* dgamma,
                                  float* dbeta, void* ws, hipStream_t stream) {
     using namespace gn;
-    Plan p = plan_of(a, true, vec_of(a, x, dy, dx));
+    Plan p = plan_of(a, true, vec_of(a, true, x, dy, dx));
     const Params q{gamma, beta, a.act};
-    float2* parts = static_cast<float2*>(ws);
+    float2* ab = static_cast<float2*>(ws);
     const int64_t rows = int64_t(a.n) * a.c * p.pieces;
-    float2* s12 = parts + rows;
-    const bool params = dgamma || dbeta;
-    if (p.held && !params) parts = nullptr;
+    float2* s12 = ab + rows;
+    Tail tail{ab, a.n, a.c, p.pieces, dgamma, dbeta, 0};
+    const unsigned last = tail_blocks(tail);
+    // a held batch of one image: the sums of its channels are the gradients
+    const bool once = p.held && a.n == 1;
+    Sums sums{ab, nullptr, nullptr};
+    if (p.held && (once || !last)) sums.ab = nullptr;
+    if (once) sums.dgamma = dgamma, sums.dbeta = dbeta;
     if (a.n > 0) {
         if (a.channels_last) {
-            if (a.dtype == DT_F16) cols_bwd<DT_F16>(p, a.n, x, dy, q, mean, rstd, dx, parts, s12, stream);
-            else cols_bwd<DT_F32>(p, a.n, x, dy, q, mean, rstd, dx, parts, s12, stream);
+            if (a.dtype == DT_F16) cols_bwd<DT_F16>(p, a.n, x, dy, q, mean, rstd, dx, sums, s12, tail, stream);
+            else cols_bwd<DT_F32>(p, a.n, x, dy, q, mean, rstd, dx, sums, s12, tail, stream);
         } else {
             p.rows.lead = int((reinterpret_cast<uintptr_t>(x) & 15u) / (a.dtype == DT_F16 ? 2 : 4));
-            if (a.dtype == DT_F16) rows_bwd<DT_F16>(p, rows, x, dy, q, mean, rstd, dx, parts, s12, stream);
-            else rows_bwd<DT_F32>(p, rows, x, dy, q, mean, rstd, dx, parts, s12, stream);
+            if (a.dtype == DT_F16) rows_bwd<DT_F16>(p, rows, x, dy, q, mean, rstd, dx, sums, s12, tail, stream);
+            else rows_bwd<DT_F32>(p, rows, x, dy, q, mean, rstd, dx, sums, s12, tail, stream);
         }
     }
-    if (params)
-        hipLaunchKernelGGL(k_gn_param, dim3(unsigned((a.c + 31) / 32)), dim3(1024), 0, stream, parts, a.n, a.c, p.pieces,
-                           dgamma, dbeta);
+    if (last && !once && (p.held || a.n == 0))
+        hipLaunchKernelGGL(k_gn_param, dim3(last), dim3(1024), 0, stream, tail);
     return hipGetLastError();
 }
 

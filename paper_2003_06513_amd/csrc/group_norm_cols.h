@@ -15,18 +15,19 @@ struct Place {
     int first, last;        // pixels of the block
     bool on;
 };
-// Blocks that are eight apart run on the same compute die, whose cache their
-// neighbouring channels share: the tiles of an image are eight apart.
+// Blocks that are eight apart run on the same compute die, whose cache holds a
+// line of memory once: the `near` tiles that share lines are eight apart.
 template <int V>
 __device__ __forceinline__ bool place(const Cols& q, int images, Place& p) {
-    const int per = 8 * q.tiles * q.chunks;
-    const int b = int(blockIdx.x);
-    const int in = b % per;
-    p.n = b / per * 8 + (in & 7);
-    if (p.n >= images) return false;
-    const int rest = in >> 3;
-    p.chunk = rest / q.tiles;
-    p.c0 = rest % q.tiles * q.tile;
+    const unsigned per = 8u * unsigned(q.near);
+    const unsigned slab = blockIdx.x / per * 8 + (blockIdx.x & 7);      // of an image, a chunk and `near` tiles
+    const unsigned wide = unsigned(q.tiles + q.near - 1) / unsigned(q.near);
+    const unsigned unit = slab / wide;
+    const int tile = int((slab - unit * wide) * unsigned(q.near) + (blockIdx.x % per >> 3));
+    p.n = int(unit / unsigned(q.chunks));
+    if (p.n >= images || tile >= q.tiles) return false;
+    p.chunk = int(unit % unsigned(q.chunks));
+    p.c0 = tile * q.tile;
     p.width = q.c - p.c0 < q.tile ? q.c - p.c0 : q.tile;
     const int cols = 1 << q.cols_log2;
     p.rel = int(threadIdx.x & unsigned(cols - 1)) * V;
@@ -93,7 +94,7 @@ __device__ __forceinline__ void each_group(const Cols& q, int count, const float
 }
 
 template <int DT, int V, int K, int ACT>
-__global__ __launch_bounds__(threads_of(V, K)) void k_gn_cols_fwd(const typename Elt<DT>::T* __restrict__ x, Cols q,
+__global__ __launch_bounds__(threads_of(DT, V, K)) void k_gn_cols_fwd(const typename Elt<DT>::T* __restrict__ x, Cols q,
                                                                   int images, Params w, float eps,
                                                                   typename Elt<DT>::T* __restrict__ y,
                                                                   float* __restrict__ mean, float* __restrict__ rstd) {
@@ -168,17 +169,23 @@ __global__ __launch_bounds__(threads_of(V, K)) void k_gn_cols_fwd(const typename
     });
 }
 
-template <int V>
-__device__ __forceinline__ void coefficients(const Cols& q, const Place& p, const Params& w, const float* mean,
-                                             const float* rstd, Coeff (&k)[V]) {
+// The mean and rstd that lie in memory, of the thread's channel j.
+__device__ __forceinline__ auto kept(const Cols& q, const Place& p, const float* mean, const float* rstd) {
+    return [&q, &p, mean, rstd](int j) {
+        const int64_t g = int64_t(p.n) * q.groups + (p.on ? group_of(q, p.c0 + p.rel + j) : 0);
+        return make_float2(mean[g], rstd[g]);
+    };
+}
+template <int V, class F>
+__device__ __forceinline__ void coefficients(const Cols& q, const Place& p, const Params& w, F stats, Coeff (&k)[V]) {
     float ga[V], be[V];
     const int c = p.c0 + p.rel;
     values<V>(w.gamma ? w.gamma + c : nullptr, p.on, 1.f, ga);
     values<V>(w.beta ? w.beta + c : nullptr, p.on, 0.f, be);
 #pragma unroll
     for (int j = 0; j < V; ++j) {
-        const int64_t g = int64_t(p.n) * q.groups + (p.on ? group_of(q, c + j) : 0);
-        k[j] = Coeff{mean[g], rstd[g], ga[j], be[j]};
+        const float2 ms = stats(j);
+        k[j] = Coeff{ms.x, ms.y, ga[j], be[j]};
     }
 }
 
@@ -215,13 +222,12 @@ __device__ __forceinline__ void write_back(const typename Pack<DT, V>::R (&d)[K]
 }
 
 template <int DT, int V, int K, int ACT>
-__global__ __launch_bounds__(threads_of(V, K)) void k_gn_cols_bwd(const typename Elt<DT>::T* __restrict__ x,
+__global__ __launch_bounds__(threads_of(DT, V, K), 4) void k_gn_cols_bwd(const typename Elt<DT>::T* __restrict__ x,
                                                                      const typename Elt<DT>::T* __restrict__ dy, Cols q,
                                                                      int images, Params w,
                                                                      const float* __restrict__ mean,
                                                                      const float* __restrict__ rstd,
-                                                                     typename Elt<DT>::T* __restrict__ dx,
-                                                                     float2* __restrict__ sums) {
+                                                                     typename Elt<DT>::T* __restrict__ dx, Sums sums) {
     using P = Pack<DT, V>;
     extern __shared__ float lds[];              // two each: the waves' sums, the channels', the groups'
     Place p;
@@ -238,7 +244,7 @@ __global__ __launch_bounds__(threads_of(V, K)) void k_gn_cols_bwd(const typename
         e[i] = get<typename P::R>(gb, byte);
     });
     Coeff k[V];
-    coefficients<V>(q, p, w, mean, rstd, k);
+    coefficients<V>(q, p, w, kept(q, p, mean, rstd), k);
     float a[V], b[V];
     sums_back<DT, V, K, ACT>(d, e, q, p, k, a, b);
     wave_channels<V>(a, q, p.width, lds);
@@ -247,7 +253,9 @@ __global__ __launch_bounds__(threads_of(V, K)) void k_gn_cols_bwd(const typename
     for (int c = threadIdx.x; c < p.width; c += blockDim.x) {
         const float2 ab = make_float2(sum_of_channel(lds, q, c), sum_of_channel(lds + all, q, c));
         ch[c] = ab.x, ch2[c] = ab.y;
-        if (sums) sums[int64_t(p.n) * q.c + p.c0 + c] = ab;
+        if (sums.ab) sums.ab[int64_t(p.n) * q.c + p.c0 + c] = ab;
+        if (sums.dgamma) sums.dgamma[p.c0 + c] = ab.y;
+        if (sums.dbeta) sums.dbeta[p.c0 + c] = ab.x;
     }
     __syncthreads();
     const float* gamma = w.gamma ? w.gamma + p.c0 : nullptr;
@@ -313,12 +321,20 @@ __global__ __launch_bounds__(256, 4) void k_gn_colparts_fwd(const typename Elt<D
             make_float4(ch[c], sum_of_channel(lds + all, q, c), num, 0.f);
 }
 
+// Calls f(group, lane) with a run of q.join_lanes lanes for each of the block's groups.
+template <class F> __device__ __forceinline__ void each_joined(const Cols& q, int count, F f) {
+    const int lane = int(threadIdx.x) & (q.join_lanes - 1);
+    for (int g = int(threadIdx.x) / q.join_lanes; g < count; g += int(blockDim.x) / q.join_lanes) f(g, lane);
+}
+
 template <int DT, int V, int K, int ACT>
 __global__ __launch_bounds__(256, 4) void k_gn_colwrite_fwd(const typename Elt<DT>::T* __restrict__ x, Cols q, int images,
-                                                         Params w, const float* __restrict__ mean,
-                                                         const float* __restrict__ rstd,
-                                                         typename Elt<DT>::T* __restrict__ y) {
+                                                            Params w, float* __restrict__ mean,
+                                                            float* __restrict__ rstd,
+                                                            const float4* __restrict__ parts, float eps,
+                                                            typename Elt<DT>::T* __restrict__ y) {
     using P = Pack<DT, V>;
+    extern __shared__ float2 joined[];          // the groups' statistics
     Place p;
     if (!place<V>(q, images, p)) return;
     const int64_t at = base_of(q, p);
@@ -326,7 +342,21 @@ __global__ __launch_bounds__(256, 4) void k_gn_colwrite_fwd(const typename Elt<D
     typename P::R d[K];
     each<DT, K>(q, p, [&](int i, uint32_t byte) { d[i] = get<typename P::R>(xb, byte); });
     Coeff k[V];
-    coefficients<V>(q, p, w, mean, rstd, k);
+    if (parts) {
+        const int64_t first = int64_t(p.n) * q.c + p.c0, g0 = int64_t(p.n) * q.groups + group_of(q, p.c0);
+        each_joined(q, group_of(q, p.width), [&](int g, int lane) {
+            const int per = q.cg * q.chunks;
+            const float2 ms = joined_stats(parts + (first * q.chunks + int64_t(g) * per), per, lane, q.join_lanes, eps);
+            if (lane == 0) {
+                joined[g] = ms;
+                if (mean && p.chunk == 0) mean[g0 + g] = ms.x, rstd[g0 + g] = ms.y;
+            }
+        });
+        __syncthreads();
+        coefficients<V>(q, p, w, [&](int j) { return joined[p.on ? group_of(q, p.rel + j) : 0]; }, k);
+    } else {
+        coefficients<V>(q, p, w, kept(q, p, mean, rstd), k);
+    }
     each<DT, K>(q, p, [&](int i, uint32_t byte) {
         float f[V];
         P::open(d[i], f);
@@ -354,7 +384,7 @@ __global__ __launch_bounds__(256, 4) void k_gn_colparts_bwd(const typename Elt<D
         e[i] = get<typename P::R>(gb, byte);
     });
     Coeff k[V];
-    coefficients<V>(q, p, w, mean, rstd, k);
+    coefficients<V>(q, p, w, kept(q, p, mean, rstd), k);
     float a[V], b[V];
     sums_back<DT, V, K, ACT>(d, e, q, p, k, a, b);
     wave_channels<V>(a, q, p.width, lds);
@@ -370,8 +400,11 @@ __global__ __launch_bounds__(256, 4) void k_gn_colwrite_bwd(const typename Elt<D
                                                          const typename Elt<DT>::T* __restrict__ dy, Cols q, int images,
                                                          Params w, const float* __restrict__ mean,
                                                          const float* __restrict__ rstd, const float2* __restrict__ s12,
+                                                         const float2* __restrict__ parts, Tail tail,
                                                          typename Elt<DT>::T* __restrict__ dx) {
     using P = Pack<DT, V>;
+    extern __shared__ float2 joined[];          // the groups' sums
+    if (blockIdx.x >= tail.first) return param_block(tail);
     Place p;
     if (!place<V>(q, images, p)) return;
     const int64_t at = base_of(q, p);
@@ -382,16 +415,30 @@ __global__ __launch_bounds__(256, 4) void k_gn_colwrite_bwd(const typename Elt<D
         e[i] = get<typename P::R>(gb, byte);
     });
     Coeff k[V];
-    coefficients<V>(q, p, w, mean, rstd, k);
+    coefficients<V>(q, p, w, kept(q, p, mean, rstd), k);
+    if (parts) {
+        const int64_t first = int64_t(p.n) * q.c + p.c0;
+        each_joined(q, group_of(q, p.width), [&](int g, int lane) {
+            const int per = q.cg * q.chunks;
+            const float2 s = joined_back(parts + (first * q.chunks + int64_t(g) * per), per, q.chunks,
+                                         w.gamma ? w.gamma + p.c0 + g * q.cg : nullptr, float(q.cg) * float(q.hw), lane,
+                                         q.join_lanes);
+            if (lane == 0) joined[g] = s;
+        });
+        __syncthreads();
+    }
     float s1[V], s2[V];
 #pragma unroll
     for (int j = 0; j < V; ++j) {
-        const int c = p.on ? p.c0 + p.rel + j : 0;
-        const float2 t = s12[int64_t(p.n) * q.groups + group_of(q, c)];
+        const int c = p.on ? p.rel + j : 0;
+        const float2 t = parts ? joined[group_of(q, c)] : s12[int64_t(p.n) * q.groups + group_of(q, p.c0 + c)];
         s1[j] = t.x, s2[j] = t.y;
     }
     write_back<DT, V, K, ACT>(d, e, q, p, k, s1, s2, dx + at);
 }
+
+// LDS of a block that joins its groups' pieces.
+unsigned joined_lds(const Plan& p) { return p.joined ? unsigned(sizeof(float2)) * unsigned(p.cols.tile / p.cols.cg) : 0u; }
 
 template <int DT, int V>
 void fwd(const Plan& p, int n, const void* x, const Params& q, float eps, void* y, float* mean, float* rstd, float4* parts,
@@ -402,47 +449,50 @@ void fwd(const Plan& p, int n, const void* x, const Params& q, float eps, void* 
     const dim3 grid(static_cast<unsigned>(p.grid)), block(static_cast<unsigned>(p.threads));
     if (p.held) {
         with_act(q.act, [&](auto act) {
-            with_count<V, false>(p.k, [&](auto k) {
+            with_count<DT, V, false>(p.k, [&](auto k) {
                 hipLaunchKernelGGL((k_gn_cols_fwd<DT, V, decltype(k)::value, decltype(act)::value>), grid, block,
                                    cols_lds(p.cols, p.threads, 1, 2), st, xt, p.cols, n, q, eps, yt, mean, rstd);
             });
         });
         return;
     }
-    constexpr int K = V == 1 ? kPieceSingle : kPiece;
+    constexpr int K = piece_of(DT, V);
     hipLaunchKernelGGL((k_gn_colparts_fwd<DT, V, K>), grid, block, cols_lds(p.cols, p.threads, 2, 1), st, xt, p.cols, n,
                        parts);
-    combine_fwd(parts, int64_t(n) * p.cols.groups, p.cols.cg * p.pieces, eps, mean, rstd, st);
+    if (!p.joined) combine_fwd(parts, int64_t(n) * p.cols.groups, p.cols.cg * p.pieces, eps, mean, rstd, st);
     with_act(q.act, [&](auto act) {
-        hipLaunchKernelGGL((k_gn_colwrite_fwd<DT, V, K, decltype(act)::value>), grid, block, 0, st, xt, p.cols, n, q, mean,
-                           rstd, yt);
+        hipLaunchKernelGGL((k_gn_colwrite_fwd<DT, V, K, decltype(act)::value>), grid, block, joined_lds(p), st, xt, p.cols, n,
+                           q, mean, rstd, p.joined ? parts : nullptr, eps, yt);
     });
 }
 
 template <int DT, int V>
 void bwd(const Plan& p, int n, const void* x, const void* dy, const Params& q, const float* mean, const float* rstd,
-         void* dx, float2* parts, float2* s12, hipStream_t st) {
+         void* dx, const Sums& sums, float2* s12, Tail tail, hipStream_t st) {
     using T = typename Elt<DT>::T;
     const T *xt = static_cast<const T*>(x), *gt = static_cast<const T*>(dy);
     T* dt = static_cast<T*>(dx);
     const dim3 grid(static_cast<unsigned>(p.grid)), block(static_cast<unsigned>(p.threads));
     if (p.held) {
         with_act(q.act, [&](auto act) {
-            with_count<V, true>(p.k, [&](auto k) {
+            with_count<DT, V, true>(p.k, [&](auto k) {
                 hipLaunchKernelGGL((k_gn_cols_bwd<DT, V, decltype(k)::value, decltype(act)::value>), grid, block,
-                                   cols_lds(p.cols, p.threads, 2, 4), st, xt, gt, p.cols, n, q, mean, rstd, dt, parts);
+                                   cols_lds(p.cols, p.threads, 2, 4), st, xt, gt, p.cols, n, q, mean, rstd, dt, sums);
             });
         });
         return;
     }
-    constexpr int K = V == 1 ? kPieceSingle : kPiece;
+    constexpr int K = piece_of(DT, V);
     with_act(q.act, [&](auto act) {
         hipLaunchKernelGGL((k_gn_colparts_bwd<DT, V, K, decltype(act)::value>), grid, block,
-                           cols_lds(p.cols, p.threads, 2, 0), st, xt, gt, p.cols, n, q, mean, rstd, parts);
-        combine_bwd(parts, int64_t(n) * p.cols.groups, p.cols.cg * p.pieces, p.pieces, p.cols.groups, p.cols.cg,
-                    float(p.cols.cg) * float(p.cols.hw), q.gamma, s12, st);
-        hipLaunchKernelGGL((k_gn_colwrite_bwd<DT, V, K, decltype(act)::value>), grid, block, 0, st, xt, gt, p.cols, n, q,
-                           mean, rstd, s12, dt);
+                           cols_lds(p.cols, p.threads, 2, 0), st, xt, gt, p.cols, n, q, mean, rstd, sums.ab);
+        if (!p.joined)
+            combine_bwd(sums.ab, int64_t(n) * p.cols.groups, p.cols.cg * p.pieces, p.pieces, p.cols.groups, p.cols.cg,
+                        float(p.cols.cg) * float(p.cols.hw), q.gamma, s12, st);
+        tail.first = grid.x;
+        hipLaunchKernelGGL((k_gn_colwrite_bwd<DT, V, K, decltype(act)::value>), dim3(grid.x + tail_blocks(tail)), block,
+                           joined_lds(p), st, xt, gt, p.cols, n, q, mean, rstd, s12, p.joined ? sums.ab : nullptr, tail,
+                           dt);
     });
 }
 
@@ -451,16 +501,16 @@ void bwd(const Plan& p, int n, const void* x, const void* dy, const Params& q, c
 template <int DT>
 void cols_fwd(const Plan& p, int n, const void* x, const Params& q, float eps, void* y, float* mean, float* rstd,
               float4* parts, hipStream_t st) {
-    constexpr int V = DT == DT_F16 ? 8 : 4;
+    constexpr int V = vector_of(DT, false);
     if (p.vec == 0) fwd<DT, 1>(p, n, x, q, eps, y, mean, rstd, parts, st);
     else fwd<DT, V>(p, n, x, q, eps, y, mean, rstd, parts, st);
 }
 template <int DT>
 void cols_bwd(const Plan& p, int n, const void* x, const void* dy, const Params& q, const float* mean, const float* rstd,
-              void* dx, float2* parts, float2* s12, hipStream_t st) {
-    constexpr int V = DT == DT_F16 ? 8 : 4;
-    if (p.vec == 0) bwd<DT, 1>(p, n, x, dy, q, mean, rstd, dx, parts, s12, st);
-    else bwd<DT, V>(p, n, x, dy, q, mean, rstd, dx, parts, s12, st);
+              void* dx, const Sums& sums, float2* s12, Tail tail, hipStream_t st) {
+    constexpr int V = vector_of(DT, true);
+    if (p.vec == 0) bwd<DT, 1>(p, n, x, dy, q, mean, rstd, dx, sums, s12, tail, st);
+    else bwd<DT, V>(p, n, x, dy, q, mean, rstd, dx, sums, s12, tail, st);
 }
 
 }  // namespace gn

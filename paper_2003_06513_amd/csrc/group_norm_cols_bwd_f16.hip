@@ -4,6 +4,6 @@
 namespace psc {
 namespace gn {
 template void cols_bwd<DT_F16>(const Plan&, int, const void*, const void*, const Params&, const float*, const float*, void*,
-                               float2*, float2*, hipStream_t);
+                               const Sums&, float2*, Tail, hipStream_t);
 }  // namespace gn
 }  // namespace psc

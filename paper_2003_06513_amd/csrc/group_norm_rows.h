@@ -36,7 +36,7 @@ struct Nothing {
 };
 
 template <int DT, int V, bool MASK, int K, int ACT>
-__global__ __launch_bounds__(threads_of(V, K)) void k_gn_rows_fwd(const typename Elt<DT>::T* __restrict__ x, Rows s,
+__global__ __launch_bounds__(threads_of(DT, V, K)) void k_gn_rows_fwd(const typename Elt<DT>::T* __restrict__ x, Rows s,
                                                                   Params q, float eps,
                                                                   typename Elt<DT>::T* __restrict__ y,
                                                                   float* __restrict__ mean, float* __restrict__ rstd) {
@@ -88,14 +88,13 @@ __global__ __launch_bounds__(threads_of(V, K)) void k_gn_rows_fwd(const typename
     }, Nothing());
 }
 
-// sums [n][c]: A and B of each row, for the parameters' gradients; may be NULL.
 template <int DT, int V, bool MASK, int K, int ACT>
-__global__ __launch_bounds__(threads_of(V, K)) void k_gn_rows_bwd(const typename Elt<DT>::T* __restrict__ x,
+__global__ __launch_bounds__(threads_of(DT, V, K)) void k_gn_rows_bwd(const typename Elt<DT>::T* __restrict__ x,
                                                                   const typename Elt<DT>::T* __restrict__ dy, Rows s,
                                                                   Params q, const float* __restrict__ mean,
                                                                   const float* __restrict__ rstd,
                                                                   typename Elt<DT>::T* __restrict__ dx,
-                                                                  float2* __restrict__ sums) {
+                                                                  Sums sums) {
     using P = Pack<DT, V>;
     extern __shared__ float2 row_params[];      // gamma and beta of the rows
     float2* row_parts = row_params + s.cg;      // [cg][waves that share a row]
@@ -145,7 +144,9 @@ __global__ __launch_bounds__(threads_of(V, K)) void k_gn_rows_bwd(const typename
             a += t.x;
             c += t.y;
         }
-        if (sums) sums[int64_t(blockIdx.x) * s.cg + row] = make_float2(a, c);
+        if (sums.ab) sums.ab[int64_t(blockIdx.x) * s.cg + row] = make_float2(a, c);
+        if (sums.dgamma) sums.dgamma[c0 + row] = c;
+        if (sums.dbeta) sums.dbeta[c0 + row] = a;
         const float ga = row_params[row].x;
         s1 = fmaf(ga, a, s1);
         s2 = fmaf(ga, c, s2);
@@ -171,7 +172,7 @@ struct Piece {
     unsigned id, row, ng;
     int c, piece;
 };
-__device__ __forceinline__ Piece piece_of(const Rows& s, int pieces) {
+__device__ __forceinline__ Piece this_piece(const Rows& s, int pieces) {
     Piece p;
     p.id = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6));
     p.row = p.id / unsigned(pieces);
@@ -197,7 +198,7 @@ template <int DT, int V, bool MASK, int K>
 __global__ __launch_bounds__(256, 4) void k_gn_rowparts_fwd(const typename Elt<DT>::T* __restrict__ x, Rows s, int pieces,
                                                          unsigned count, float4* __restrict__ parts) {
     using P = Pack<DT, V>;
-    const Piece p = piece_of(s, pieces);
+    const Piece p = this_piece(s, pieces);
     if (p.id >= count) return;
     const Base<V, MASK> b(s, int64_t(p.row) * s.hw);
     const int skip = p.piece * K * 64;
@@ -235,17 +236,26 @@ __device__ __forceinline__ Coeff coeff_of(const Piece& p, const Params& q, const
 
 template <int DT, int V, bool MASK, int K, int ACT>
 __global__ __launch_bounds__(256, 4) void k_gn_rowwrite_fwd(const typename Elt<DT>::T* __restrict__ x, Rows s, Params q,
-                                                         int pieces, unsigned count, const float* __restrict__ mean,
-                                                         const float* __restrict__ rstd,
-                                                         typename Elt<DT>::T* __restrict__ y) {
+                                                            int pieces, unsigned count, float* __restrict__ mean,
+                                                            float* __restrict__ rstd,
+                                                            const float4* __restrict__ parts, float eps,
+                                                            typename Elt<DT>::T* __restrict__ y) {
     using P = Pack<DT, V>;
-    const Piece p = piece_of(s, pieces);
+    const Piece p = this_piece(s, pieces);
     if (p.id >= count) return;
     const Base<V, MASK> b(s, int64_t(p.row) * s.hw);
     const int skip = p.piece * K * 64;
     typename P::R d[K];
     each_of_piece<V, MASK, K>(s, b, skip, [&](int i, const Window& w, bool) { d[i] = load<DT, V, MASK>(x, b, w); });
-    const Coeff k = coeff_of(p, q, mean, rstd);
+    Coeff k{0.f, 0.f, or_one(q.gamma, p.c), or_zero(q.beta, p.c)};
+    if (parts) {
+        const int per = s.cg * pieces;
+        const float2 ms = joined_stats(parts + int64_t(p.ng) * per, per, int(threadIdx.x & 63), 64, eps);
+        k.mu = ms.x, k.r = ms.y;
+        if (mean && p.id == p.ng * unsigned(per) && (threadIdx.x & 63) == 0) mean[p.ng] = k.mu, rstd[p.ng] = k.r;
+    } else {
+        k.mu = mean[p.ng], k.r = rstd[p.ng];
+    }
     each_of_piece<V, MASK, K>(s, b, skip, [&](int i, const Window& w, bool on) {
         float f[V];
         P::open(d[i], f);
@@ -261,7 +271,7 @@ __global__ __launch_bounds__(256, 4) void k_gn_rowparts_bwd(const typename Elt<D
                                                          int pieces, unsigned count, const float* __restrict__ mean,
                                                          const float* __restrict__ rstd, float2* __restrict__ parts) {
     using P = Pack<DT, V>;
-    const Piece p = piece_of(s, pieces);
+    const Piece p = this_piece(s, pieces);
     if (p.id >= count) return;
     const Base<V, MASK> b(s, int64_t(p.row) * s.hw);
     const int skip = p.piece * K * 64;
@@ -296,9 +306,11 @@ __global__ __launch_bounds__(256, 4) void k_gn_rowwrite_bwd(const typename Elt<D
                                                          const typename Elt<DT>::T* __restrict__ dy, Rows s, Params q,
                                                          int pieces, unsigned count, const float* __restrict__ mean,
                                                          const float* __restrict__ rstd, const float2* __restrict__ s12,
+                                                         const float2* __restrict__ parts, Tail tail,
                                                          typename Elt<DT>::T* __restrict__ dx) {
     using P = Pack<DT, V>;
-    const Piece p = piece_of(s, pieces);
+    if (blockIdx.x >= tail.first) return param_block(tail);
+    const Piece p = this_piece(s, pieces);
     if (p.id >= count) return;
     const Base<V, MASK> b(s, int64_t(p.row) * s.hw);
     const int skip = p.piece * K * 64;
@@ -308,7 +320,10 @@ __global__ __launch_bounds__(256, 4) void k_gn_rowwrite_bwd(const typename Elt<D
         e[i] = load<DT, V, MASK>(dy, b, w);
     });
     const Coeff k = coeff_of(p, q, mean, rstd);
-    const float2 sum = s12[p.ng];
+    const int per = s.cg * pieces;
+    const float2 sum = parts ? joined_back(parts + int64_t(p.ng) * per, per, pieces, q.gamma ? q.gamma + p.c / s.cg * s.cg : nullptr,
+                                           float(s.cg) * float(s.hw), int(threadIdx.x & 63), 64)
+                             : s12[p.ng];
     each_of_piece<V, MASK, K>(s, b, skip, [&](int i, const Window& w, bool on) {
         float f[V], g[V];
         P::open(d[i], f);
@@ -330,27 +345,27 @@ void fwd(const Plan& p, int64_t count, const void* x, const Params& q, float eps
             const dim3 grid(static_cast<unsigned>(p.grid)), block(static_cast<unsigned>(p.threads));
             const unsigned lds = unsigned(sizeof(float2)) * unsigned(p.rows.cg);
             with_act(q.act, [&](auto act) {
-                with_count<V, false>(p.k, [&](auto k) {
+                with_count<DT, V, false>(p.k, [&](auto k) {
                     hipLaunchKernelGGL((k_gn_rows_fwd<DT, V, MASK, decltype(k)::value, decltype(act)::value>), grid, block,
                                        lds, st, xt, p.rows, q, eps, yt, mean, rstd);
                 });
             });
             return;
         }
-    constexpr int K = V == 1 ? kPieceSingle : kPiece;
+    constexpr int K = piece_of(DT, V);
     const dim3 grid(static_cast<unsigned>((count + 3) / 4));
     hipLaunchKernelGGL((k_gn_rowparts_fwd<DT, V, MASK, K>), grid, dim3(256), 0, st, xt, p.rows, p.pieces, unsigned(count),
                        parts);
-    combine_fwd(parts, count / (int64_t(p.rows.cg) * p.pieces), p.rows.cg * p.pieces, eps, mean, rstd, st);
+    if (!p.joined) combine_fwd(parts, count / (int64_t(p.rows.cg) * p.pieces), p.rows.cg * p.pieces, eps, mean, rstd, st);
     with_act(q.act, [&](auto act) {
         hipLaunchKernelGGL((k_gn_rowwrite_fwd<DT, V, MASK, K, decltype(act)::value>), grid, dim3(256), 0, st, xt, p.rows, q,
-                           p.pieces, unsigned(count), mean, rstd, yt);
+                           p.pieces, unsigned(count), mean, rstd, p.joined ? parts : nullptr, eps, yt);
     });
 }
 
 template <int DT, int V, bool MASK>
 void bwd(const Plan& p, int64_t count, const void* x, const void* dy, const Params& q, const float* mean,
-         const float* rstd, void* dx, float2* parts, float2* s12, hipStream_t st) {
+         const float* rstd, void* dx, const Sums& sums, float2* s12, Tail tail, hipStream_t st) {
     using T = typename Elt<DT>::T;
     const T *xt = static_cast<const T*>(x), *gt = static_cast<const T*>(dy);
     T* dt = static_cast<T*>(dx);
@@ -360,23 +375,26 @@ void bwd(const Plan& p, int64_t count, const void* x, const void* dy, const Para
             const int lanes = 1 << p.rows.lanes_log2;
             const unsigned lds = unsigned(sizeof(float2)) * unsigned(p.rows.cg) * unsigned(1 + (lanes > 64 ? lanes / 64 : 1));
             with_act(q.act, [&](auto act) {
-                with_count<V, true>(p.k, [&](auto k) {
+                with_count<DT, V, true>(p.k, [&](auto k) {
                     hipLaunchKernelGGL((k_gn_rows_bwd<DT, V, MASK, decltype(k)::value, decltype(act)::value>), grid, block,
-                                       lds, st, xt, gt, p.rows, q, mean, rstd, dt, parts);
+                                       lds, st, xt, gt, p.rows, q, mean, rstd, dt, sums);
                 });
             });
             return;
         }
-    constexpr int K = V == 1 ? kPieceSingle : kPiece;
+    constexpr int K = piece_of(DT, V);
     const dim3 grid(static_cast<unsigned>((count + 3) / 4));
     with_act(q.act, [&](auto act) {
         hipLaunchKernelGGL((k_gn_rowparts_bwd<DT, V, MASK, K, decltype(act)::value>), grid, dim3(256), 0, st, xt, gt,
-                           p.rows, q, p.pieces, unsigned(count), mean, rstd, parts);
+                           p.rows, q, p.pieces, unsigned(count), mean, rstd, sums.ab);
         const float m = float(p.rows.cg) * float(p.rows.hw);
-        combine_bwd(parts, count / (int64_t(p.rows.cg) * p.pieces), p.rows.cg * p.pieces, p.pieces, p.rows.groups,
-                    p.rows.cg, m, q.gamma, s12, st);
-        hipLaunchKernelGGL((k_gn_rowwrite_bwd<DT, V, MASK, K, decltype(act)::value>), grid, dim3(256), 0, st, xt, gt,
-                           p.rows, q, p.pieces, unsigned(count), mean, rstd, s12, dt);
+        if (!p.joined)
+            combine_bwd(sums.ab, count / (int64_t(p.rows.cg) * p.pieces), p.rows.cg * p.pieces, p.pieces, p.rows.groups,
+                        p.rows.cg, m, q.gamma, s12, st);
+        tail.first = grid.x;
+        hipLaunchKernelGGL((k_gn_rowwrite_bwd<DT, V, MASK, K, decltype(act)::value>), dim3(grid.x + tail_blocks(tail)),
+                           dim3(256), 0, st, xt, gt, p.rows, q, p.pieces, unsigned(count), mean, rstd, s12,
+                           p.joined ? sums.ab : nullptr, tail, dt);
     });
 }
 
@@ -385,18 +403,18 @@ void bwd(const Plan& p, int64_t count, const void* x, const void* dy, const Para
 template <int DT>
 void rows_fwd(const Plan& p, int64_t count, const void* x, const Params& q, float eps, void* y, float* mean, float* rstd,
               float4* parts, hipStream_t st) {
-    constexpr int V = DT == DT_F16 ? 8 : 4;
+    constexpr int V = vector_of(DT, false);
     if (p.vec == 0) fwd<DT, 1, false>(p, count, x, q, eps, y, mean, rstd, parts, st);
     else if (p.vec == 1) fwd<DT, V, false>(p, count, x, q, eps, y, mean, rstd, parts, st);
     else fwd<DT, V, true>(p, count, x, q, eps, y, mean, rstd, parts, st);
 }
 template <int DT>
 void rows_bwd(const Plan& p, int64_t count, const void* x, const void* dy, const Params& q, const float* mean,
-              const float* rstd, void* dx, float2* parts, float2* s12, hipStream_t st) {
-    constexpr int V = DT == DT_F16 ? 8 : 4;
-    if (p.vec == 0) bwd<DT, 1, false>(p, count, x, dy, q, mean, rstd, dx, parts, s12, st);
-    else if (p.vec == 1) bwd<DT, V, false>(p, count, x, dy, q, mean, rstd, dx, parts, s12, st);
-    else bwd<DT, V, true>(p, count, x, dy, q, mean, rstd, dx, parts, s12, st);
+              const float* rstd, void* dx, const Sums& sums, float2* s12, Tail tail, hipStream_t st) {
+    constexpr int V = vector_of(DT, false);
+    if (p.vec == 0) bwd<DT, 1, false>(p, count, x, dy, q, mean, rstd, dx, sums, s12, tail, st);
+    else if (p.vec == 1) bwd<DT, V, false>(p, count, x, dy, q, mean, rstd, dx, sums, s12, tail, st);
+    else bwd<DT, V, true>(p, count, x, dy, q, mean, rstd, dx, sums, s12, tail, st);
 }
 
 }  // namespace gn
