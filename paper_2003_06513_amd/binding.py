@@ -738,7 +738,7 @@ def group_norm_bwd(x, dy, groups: int, gamma, beta, mean, rstd, dx, dgamma=None,
 
 # ------------------------------------------------------------------ the optimiser
 GRAD_NORM_WS_BYTES = 8192
-ADAMW_STATE_BYTES = 64
+ADAMW_STATE_BYTES = 4352
 ADAMW_GROUP = 256           # elements that share the scales of 8-bit moments
 
 
@@ -829,7 +829,7 @@ def grad_norm(params: ParamList, out, max_norm: float = float("inf"), scale: flo
 
 def adamw_step(params: ParamList, state, lr, betas=(0.9, 0.999), eps: float = 1e-8, factor=None, stream=None):
     """psc_adamw_step: one step on every tensor of the list.  ``state``: a
-    device tensor of 64 bytes, zeros before the first step; ``lr``: a number,
+    device tensor of ADAMW_STATE_BYTES bytes, zeros before the first step; ``lr``: a number,
     or an fp32 device tensor that the step reads; ``factor``: None, or an fp32
     device tensor whose first element the gradients are multiplied by."""
     params.check_device()

@@ -178,7 +178,7 @@ struct AdamwArgs {
     float lr, beta1, beta2, eps;
     const float* d_lr;
 };
-constexpr size_t kAdamwStateBytes = 64;
+constexpr size_t kAdamwStateBytes = 4352;
 size_t grad_norm_workspace_bytes();
 hipError_t launch_grad_norm(const ParamView* q, int count, float scale, float max_norm, float* out, void* ws,
                             hipStream_t stream);

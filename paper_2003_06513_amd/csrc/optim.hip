@@ -24,8 +24,10 @@ typedef int8_t c4 __attribute__((ext_vector_type(4)));
 typedef uint8_t b4 __attribute__((ext_vector_type(4)));
 
 // A table of tensors as a kernel argument (the arguments of a launch stay
-// under 4 KiB).
-constexpr int kMaxEntries = 52;
+// under 4 KiB).  Chunks of 1024 elements are numbered through the table, and a
+// block of a step takes one: blocks that go on to other chunks were slower (64
+// x 512 x 512 x 9 with 32 bits 869 us, not 783), as were chunks of 2048 (802).
+constexpr int kMaxEntries = 62;
 constexpr int kGroup = 256;       // elements that share the scales of 8-bit moments: 4 per lane of a wave
 constexpr int kNormBlocks = 1024; // partial sums of the norm (fixed: deterministic order)
 
@@ -38,67 +40,95 @@ struct Entry {
     void* m;
     void* v;
     float2* scale;
-    int64_t numel;
+    uint32_t numel;
     float wd;
+    int32_t first;       // the tensor's first chunk
     uint32_t flags;      // kWide: every pointer is aligned for four elements
 };
 struct Table {
     Entry e[kMaxEntries];
-    int32_t first[kMaxEntries + 1];   // first chunk of each tensor; [n]: the number of chunks
-    int32_t n;
+    int32_t n, chunks;
 };
 
 struct GradEntry {
     const void* g;
-    int64_t numel;
-    uint32_t flags;
-    int32_t first;
+    uint32_t numel;
+    uint32_t first;      // and in the two bits above 30 the flags
 };
-constexpr int kMaxGrads = 160;
+constexpr int kMaxGrads = 240;
 struct GradTable {
     GradEntry e[kMaxGrads];
-    int32_t chunks;
-    int32_t n;
+    int32_t n, chunks;
 };
+static_assert(sizeof(Table) <= 4000 && sizeof(GradTable) <= 4000, "kernel arguments");
 
-// What a step reads besides the tensors: worked out once on the device, in
-// 64 bits, from the count of steps.  In the caller's state, behind the count.
-struct Ctl {
+// The caller's state.  The last block of a step's last launch to read the
+// count raises it.  The blocks are counted at kEnds words, each in a line of
+// its own, and the last ones of those at one more (additions to one word take
+// 9 ns each: 20 us for 2149 blocks).  All are zero between steps.
+constexpr int kEnds = 32;
+struct alignas(128) Line {
+    uint32_t ended;
+};
+struct State {
     int64_t steps;
-    float rate;       // lr / (1 - b1^t)
-    float root;       // 1 / sqrt(1 - b2^t)
-    float lr;
-    float factor;
-    int32_t go;       // 0: the factor is not finite, and nothing is changed
-    int32_t pad;
+    Line all, some[kEnds];
 };
-static_assert(sizeof(Ctl) <= kAdamwStateBytes, "the caller's state holds it");
+static_assert(sizeof(State) <= kAdamwStateBytes, "the caller's state holds it");
 
-__global__ void k_adamw_begin(Ctl* __restrict__ ctl, const float* __restrict__ factor, const float* __restrict__ d_lr,
-                              float lr, float b1, float b2) {
-    const float f = factor ? *factor : 1.f;
-    const bool go = __builtin_isfinite(f);
-    const int64_t t = ctl->steps + 1;
-    if (d_lr) lr = *d_lr;
-    ctl->go = go;
-    if (!go) return;
-    ctl->steps = t;
-    ctl->lr = lr;
-    ctl->factor = f;
-    ctl->rate = float(double(lr) / (1.0 - pow(double(b1), double(t))));
-    ctl->root = float(1.0 / sqrt(1.0 - pow(double(b2), double(t))));
+struct Hyper {
+    float b1, b2, c1, c2, eps, lr;      // c = 1 - b
+    float ln1, ln2;                     // log b
+    const float* d_lr;
+    const float* factor;
+};
+__device__ __forceinline__ bool last_of(Line& line, uint32_t count) {
+    if (atomicAdd(&line.ended, 1u) != count - 1) return false;
+    atomicExch(&line.ended, 0u);
+    return true;
+}
+// What a step takes from the count of steps and from device memory.  1 - b^t
+// is -expm1(t log b): nothing cancels where b^t is near one.  One wave works
+// it out for the block.
+struct Now {
+    float factor, rate, root, lr;
+    bool go;             // the factor is finite; else nothing is changed
+};
+__device__ __forceinline__ Now now(const Hyper& hp, State* st, bool last) {
+    __shared__ float both[2];
+    Now n;
+    n.factor = hp.factor ? *hp.factor : 1.f;
+    n.go = __builtin_isfinite(n.factor);
+    n.lr = hp.d_lr ? *hp.d_lr : hp.lr;
+    int64_t steps = 0;
+    if (threadIdx.x < 64) {
+        steps = st->steps;
+        const float t = float(steps + 1);
+        const float rate = n.lr / -expm1f(t * hp.ln1), root = 1.f / sqrtf(-expm1f(t * hp.ln2));
+        if (threadIdx.x == 0) both[0] = rate, both[1] = root;
+    }
+    __syncthreads();
+    n.rate = both[0];
+    n.root = both[1];
+    // the block has read the count: behind the barrier, that waited for what came of it
+    if (last && n.go && threadIdx.x == 0) {
+        const uint32_t at = blockIdx.x % kEnds, blocks = gridDim.x;
+        if (last_of(st->some[at], (blocks - at + kEnds - 1) / kEnds) && last_of(st->all, blocks < kEnds ? blocks : kEnds))
+            st->steps = steps + 1;
+    }
+    return n;
 }
 
 // The entry whose chunks hold chunk c.
-__device__ __forceinline__ int find_entry(const int32_t* first, int n, int c) {
-    int lo = 0, hi = n;
+template <class E> __device__ __forceinline__ uint32_t first_of(const E& e) { return uint32_t(e.first) & 0x3fffffffu; }
+template <class T> __device__ __forceinline__ int find_entry(const T& tab, uint32_t c) {
+    int lo = 0, hi = tab.n;
     while (hi - lo > 1) {
         const int mid = (lo + hi) >> 1;
-        if (first[mid] <= c) lo = mid; else hi = mid;
+        if (first_of(tab.e[mid]) <= c) lo = mid; else hi = mid;
     }
     return lo;
 }
-
 __device__ __forceinline__ f4 load_f32(const float* p, int left, bool wide) {
     if (wide && left >= 4) return *reinterpret_cast<const f4*>(p);
     f4 r = {0.f, 0.f, 0.f, 0.f};
@@ -148,10 +178,6 @@ __device__ __forceinline__ f4 load_grad(const void* g, int64_t i, int left, uint
     return r;
 }
 
-struct Hyper {
-    float b1, b2, c1, c2, eps;      // c = 1 - b
-};
-
 // p from the new moments.  The quotient by v_rcp_f32 and v_sqrt_f32, each
 // within one unit in the last place: the step is at most a few 2^-23 of
 // itself off, far below the rounding of p.
@@ -161,29 +187,31 @@ __device__ __forceinline__ float updated(float p, float m, float v, float decay,
     return fmaf(-rate * m, __builtin_amdgcn_rcpf(d), q);
 }
 
-// One chunk of 1024 elements per block, four in a row per lane.
-__global__ __launch_bounds__(256) void k_adamw32(Table tab, Hyper hp, const Ctl* __restrict__ ctl) {
-    if (!ctl->go) return;
-    const int c = blockIdx.x;
-    const int at = find_entry(tab.first, tab.n, c);
-    const Entry& e = tab.e[at];
-    const int64_t i = int64_t(c - tab.first[at]) * 1024 + threadIdx.x * 4;
-    const int64_t rest = e.numel - i;
-    if (rest <= 0) return;
-    const int left = rest < 4 ? int(rest) : 4;
+// A step of nothing.
+__global__ void k_adamw_none(const float* __restrict__ factor, State* __restrict__ st) {
+    if (!factor || __builtin_isfinite(*factor)) st->steps = st->steps + 1;
+}
+
+// Four elements in a row per lane.
+__global__ __launch_bounds__(256) void k_adamw32(Table tab, Hyper hp, State* __restrict__ st, bool last) {
+    const Entry& e = tab.e[find_entry(tab, blockIdx.x)];
+    const uint32_t i = (blockIdx.x - first_of(e)) * 1024 + threadIdx.x * 4;
+    const int left = i >= e.numel ? 0 : e.numel - i < 4 ? int(e.numel - i) : 4;
     const bool wide = e.flags & kWide;
-    const float factor = ctl->factor, rate = ctl->rate, root = ctl->root, decay = ctl->lr * e.wd;
     float* mp = static_cast<float*>(e.m) + i;
     float* vp = static_cast<float*>(e.v) + i;
     const f4 g = load_grad(e.g, i, left, e.flags);
     f4 p = load_f32(e.p + i, left, wide), m = load_f32(mp, left, wide), v = load_f32(vp, left, wide);
+    const Now n = now(hp, st, last);        // while those are on their way
+    if (!n.go) return;
+    const float decay = n.lr * e.wd;
     h4 h;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-        const float gj = g[j] * factor;
+        const float gj = g[j] * n.factor;
         m[j] = fmaf(hp.b1, m[j], hp.c1 * gj);
         v[j] = fmaf(hp.b2, v[j], hp.c2 * (gj * gj));
-        p[j] = updated(p[j], m[j], v[j], decay, rate, root, hp.eps);
+        p[j] = updated(p[j], m[j], v[j], decay, n.rate, n.root, hp.eps);
         h[j] = Elt<DT_F16>::from_f(p[j]);
     }
     store_f32(e.p + i, p, left, wide);
@@ -205,22 +233,24 @@ __global__ __launch_bounds__(256) void k_adamw32(Table tab, Hyper hp, const Ctl*
 // with code 0 the next step would divide by eps alone.
 constexpr double kTopM = 127.0 * 127.0, kTopV = 255.0 * 255.0 * 255.0 * 255.0;
 
-__device__ __forceinline__ double decode_m(int q, double a) { return double(q * (q < 0 ? -q : q)) * (a * (1.0 / kTopM)); }
-__device__ __forceinline__ double decode_v(uint32_t c, double a) {
+// q |q| and c^4, which times the scale and 1 / kTop are the values.
+__device__ __forceinline__ double power_m(int q) { return double(q * (q < 0 ? -q : q)); }
+__device__ __forceinline__ double power_v(uint32_t c) {
     const uint32_t s = c * c;
-    return double(s * s) * (a * (1.0 / kTopV));
+    return double(s * s);
 }
 // The root is raised by more than its error, so that the code is right or one
-// too high; one look at the border below tells which.
+// too high; one look at the border below (its square is exact in fp32) tells which.
 __device__ __forceinline__ int encode_m(double t) {
     int c = int(fmaf(__builtin_amdgcn_sqrtf(float(t)), 1.f + 0x1p-20f, 0.5f));
-    const double b = double(c) - 0.5;
-    c -= c > 0 && b * b > t;
+    const float b = float(c) - 0.5f;
+    c -= c > 0 && double(b * b) > t;
     return c > 127 ? 127 : c;
 }
 __device__ __forceinline__ int encode_v(double t) {
     int c = int(fmaf(__builtin_amdgcn_sqrtf(__builtin_amdgcn_sqrtf(float(t))), 1.f + 0x1p-20f, 0.5f));
-    const double b = double(c) - 0.5, bb = b * b;
+    const float b = float(c) - 0.5f;
+    const double bb = double(b * b);
     c -= c > 0 && bb * bb > t;
     return c > 255 ? 255 : c;
 }
@@ -237,35 +267,34 @@ __device__ __forceinline__ float wave_peak(uint32_t bits) {
 __device__ __forceinline__ uint32_t magnitude_bits(float x) { return __builtin_bit_cast(uint32_t, x) & 0x7fffffffu; }
 
 // One group per wave: lane l has the elements 4 l .. 4 l + 3 of it.
-__global__ __launch_bounds__(256) void k_adamw8(Table tab, Hyper hp, const Ctl* __restrict__ ctl) {
-    if (!ctl->go) return;
-    const int c = blockIdx.x;
-    const int at = find_entry(tab.first, tab.n, c);
-    const Entry& e = tab.e[at];
-    const int64_t group = int64_t(c - tab.first[at]) * 4 + (threadIdx.x >> 6);
-    const int64_t i = group * kGroup + (threadIdx.x & 63) * 4;
-    if (group * kGroup >= e.numel) return;      // the whole wave
-    const int64_t rest = e.numel - i;
-    const int left = rest < 0 ? 0 : rest < 4 ? int(rest) : 4;
+__global__ __launch_bounds__(256) void k_adamw8(Table tab, Hyper hp, State* __restrict__ st, bool last) {
+    const Entry& e = tab.e[find_entry(tab, blockIdx.x)];
+    const uint32_t group = (blockIdx.x - first_of(e)) * 4 + (threadIdx.x >> 6), lane4 = (threadIdx.x & 63) * 4;
+    const uint32_t i = group * kGroup + lane4;
+    const int left = i >= e.numel ? 0 : e.numel - i < 4 ? int(e.numel - i) : 4;
     const bool wide = e.flags & kWide;
-    const float rate = ctl->rate, root = ctl->root, decay = ctl->lr * e.wd;
-    const double factor = ctl->factor, b1 = hp.b1, b2 = hp.b2;
     int8_t* mp = static_cast<int8_t*>(e.m) + i;
     uint8_t* vp = static_cast<uint8_t*>(e.v) + i;
-    const float2 peak = e.scale[group];
+    const float2 peak = group * kGroup < e.numel ? e.scale[group] : make_float2(0.f, 0.f);
     const f4 g = load_grad(e.g, i, left, e.flags);
     f4 p = load_f32(e.p + i, left, wide);
     c4 qm = load4<c4>(mp, left, wide);
     b4 qv = load4<b4>(vp, left, wide);
+    const Now n = now(hp, st, last);        // while those are on their way
+    if (!n.go || group * kGroup >= e.numel) return;     // the whole wave
+    const float decay = n.lr * e.wd;
+    const double factor = n.factor;
+    const double km = hp.b1 * (1.0 / kTopM) * peak.x, kv = hp.b2 * (1.0 / kTopV) * peak.y,
+                 kg = (1.0 - hp.b1) * factor, kgg = (1.0 - hp.b2) * factor * factor;
     double m[4], v[4];
     uint32_t top_m = 0, top_v = 0;
     h4 h;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-        const double gj = double(g[j]) * factor;
-        m[j] = b1 * decode_m(qm[j], peak.x) + (1.0 - b1) * gj;
-        v[j] = b2 * decode_v(qv[j], peak.y) + (1.0 - b2) * (gj * gj);
-        p[j] = updated(p[j], float(m[j]), float(v[j]), decay, rate, root, hp.eps);
+        const double gj = g[j];
+        m[j] = fma(power_m(qm[j]), km, gj * kg);
+        v[j] = fma(power_v(qv[j]), kv, gj * gj * kgg);
+        p[j] = updated(p[j], float(m[j]), float(v[j]), decay, n.rate, n.root, hp.eps);
         h[j] = Elt<DT_F16>::from_f(p[j]);
         if (j < left) {
             const uint32_t bm = magnitude_bits(float(m[j])), bv = magnitude_bits(float(v[j]));
@@ -285,7 +314,7 @@ __global__ __launch_bounds__(256) void k_adamw8(Table tab, Hyper hp, const Ctl* 
     }
     store4<c4>(mp, qm, left, wide);
     store4<b4>(vp, qv, left, wide);
-    if ((threadIdx.x & 63) == 0) e.scale[group] = make_float2(am, av);
+    if (lane4 == 0) e.scale[group] = make_float2(am, av);
 }
 
 // The moments that codes stand for: whole groups, four elements per lane.
@@ -302,15 +331,19 @@ __global__ __launch_bounds__(256) void k_moments(const int8_t* __restrict__ qm, 
     f4 x, y;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-        x[j] = float(decode_m(a[j], peak.x));
-        y[j] = float(decode_v(b[j], peak.y));
+        x[j] = float(power_m(a[j]) * (peak.x * (1.0 / kTopM)));
+        y[j] = float(power_v(b[j]) * (peak.y * (1.0 / kTopV)));
     }
     store_f32(m + i, x, left, wide);
     store_f32(v + i, y, left, wide);
 }
 
-// ---- the norm: squares in 64 bits, so that no finite gradient overflows or
-// vanishes; one partial sum per block, added in a fixed order.
+// ---- the norm.  No finite gradient's square overflows or vanishes: an fp32
+// one is squared in 64 bits; an fp16 one has an exact square in 32, of which
+// four are added there (two roundings, at most 2^-23 of their sum: a
+// conversion to 64 bits takes four times as long as another operation, and
+// with one for every element 64 x 512 x 512 x 9 took 164 us).  Sums in 64
+// bits; one partial sum per block, added in a fixed order.
 __device__ __forceinline__ double block_sum(double x) {
     __shared__ double part[4];
 #pragma unroll
@@ -322,19 +355,22 @@ __device__ __forceinline__ double block_sum(double x) {
 
 __global__ __launch_bounds__(256) void k_norm_parts(GradTable tab, bool add, double* __restrict__ part) {
     double acc = 0.0;
-    for (int c = blockIdx.x; c < tab.chunks; c += gridDim.x) {
-        int lo = 0, hi = tab.n;
-        while (hi - lo > 1) {
-            const int mid = (lo + hi) >> 1;
-            if (tab.e[mid].first <= c) lo = mid; else hi = mid;
-        }
-        const GradEntry& e = tab.e[lo];
-        const int64_t i = int64_t(c - e.first) * 1024 + threadIdx.x * 4;
-        const int64_t rest = e.numel - i;
-        if (rest <= 0) continue;
-        const f4 g = load_grad(e.g, i, rest < 4 ? int(rest) : 4, e.flags);
+    // the block's chunks lie side by side, so that it goes through the table once
+    const uint32_t chunks = uint32_t(tab.chunks), per = (chunks + gridDim.x - 1) / gridDim.x;
+    const uint32_t c0 = blockIdx.x * per, c1 = c0 + per < chunks ? c0 + per : chunks;
+    int at = c0 < c1 ? find_entry(tab, c0) : 0;
+    for (uint32_t c = c0; c < c1; ++c) {
+        if (at + 1 < tab.n && first_of(tab.e[at + 1]) == c) ++at;      // every tensor of the table has a chunk
+        const GradEntry& e = tab.e[at];
+        const uint32_t i = (c - first_of(e)) * 1024 + threadIdx.x * 4, flags = e.first >> 30;
+        if (i >= e.numel) continue;
+        const f4 g = load_grad(e.g, i, e.numel - i < 4 ? int(e.numel - i) : 4, flags);
+        if (flags & kGradF16) {
+            acc += double(fmaf(g[1], g[1], g[0] * g[0]) + fmaf(g[3], g[3], g[2] * g[2]));
+        } else {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) acc = fma(double(g[j]), double(g[j]), acc);
+            for (int j = 0; j < 4; ++j) acc = fma(double(g[j]), double(g[j]), acc);
+        }
     }
     acc = block_sum(acc);
     if (threadIdx.x == 0) part[blockIdx.x] = add ? part[blockIdx.x] + acc : acc;
@@ -365,22 +401,23 @@ uint32_t grad_flags(const ParamView& q) {
 
 size_t grad_norm_workspace_bytes() { return size_t(kNormBlocks) * sizeof(double); }
 
+namespace {
+// Tables are filled up to their room and to 2^29 chunks.
+constexpr int64_t kMaxChunks = int64_t(1) << 29;
+int64_t chunks_of(const ParamView& q) { return (q.numel + 1023) / 1024; }
+template <class T> bool full(const T& tab, int room, int64_t more) { return tab.n == room || tab.chunks + more > kMaxChunks; }
+}  // namespace
+
 hipError_t launch_grad_norm(const ParamView* q, int count, float scale, float max_norm, float* out, void* ws,
                             hipStream_t stream) {
     double* part = static_cast<double*>(ws);
-    int64_t most = 1;       // chunks of the largest launch: every launch of the call has one grid
-    int64_t sum = 0;
-    int in = 0;
-    for (int i = 0; i < count; ++i) {
-        const int64_t ch = (q[i].numel + 1023) / 1024;
-        if (ch == 0) continue;
-        if (in == kMaxGrads || sum + ch > (int64_t(1) << 30)) sum = 0, in = 0;
-        sum += ch, ++in;
-        most = sum > most ? sum : most;
-    }
-    const int grid = int(most < kNormBlocks ? most : kNormBlocks);
     GradTable tab;
     tab.n = 0, tab.chunks = 0;
+    // Every launch of the call writes or adds the same partial sums: as many as
+    // the chunks of all tensors, as far as there is room.
+    int64_t all = 0;
+    for (int i = 0; i < count; ++i) all += chunks_of(q[i]);
+    const int grid = int(all < 1 ? 1 : all < kNormBlocks ? all : kNormBlocks);
     bool add = false;
     const auto flush = [&] {
         hipLaunchKernelGGL(k_norm_parts, dim3(unsigned(grid)), dim3(256), 0, stream, tab, add, part);
@@ -388,10 +425,10 @@ hipError_t launch_grad_norm(const ParamView* q, int count, float scale, float ma
         tab.n = 0, tab.chunks = 0;
     };
     for (int i = 0; i < count; ++i) {
-        const int64_t ch = (q[i].numel + 1023) / 1024;
+        const int64_t ch = chunks_of(q[i]);
         if (ch == 0) continue;
-        if (tab.n == kMaxGrads || tab.chunks + ch > (int64_t(1) << 30)) flush();
-        tab.e[tab.n++] = GradEntry{q[i].grad, q[i].numel, grad_flags(q[i]), tab.chunks};
+        if (full(tab, kMaxGrads, ch)) flush();
+        tab.e[tab.n++] = GradEntry{q[i].grad, uint32_t(q[i].numel), uint32_t(tab.chunks) | grad_flags(q[i]) << 30};
         tab.chunks += int32_t(ch);
     }
     if (tab.n || !add) flush();
@@ -401,33 +438,38 @@ hipError_t launch_grad_norm(const ParamView* q, int count, float scale, float ma
 
 hipError_t launch_adamw(const ParamView* q, int count, const AdamwArgs& a, const float* factor, void* state,
                         hipStream_t stream) {
-    Ctl* ctl = static_cast<Ctl*>(state);
-    hipLaunchKernelGGL(k_adamw_begin, dim3(1), dim3(1), 0, stream, ctl, factor, a.d_lr, a.lr, a.beta1, a.beta2);
-    const Hyper hp{a.beta1, a.beta2, float(1.0 - double(a.beta1)), float(1.0 - double(a.beta2)), a.eps};
+    State* st = static_cast<State*>(state);
+    const Hyper hp{a.beta1, a.beta2, float(1.0 - double(a.beta1)), float(1.0 - double(a.beta2)), a.eps, a.lr,
+                   float(std::log(double(a.beta1))), float(std::log(double(a.beta2))), a.d_lr, factor};
+    int64_t left[2] = {0, 0};       // tensors that are not in a table yet: 32 bits, 8 bits
+    for (int i = 0; i < count; ++i)
+        if (q[i].numel) ++left[q[i].state_bits == 8];
+    Table tab;
+    tab.n = 0, tab.chunks = 0;
+    const auto flush = [&](int bits) {
+        const dim3 grid(unsigned(tab.chunks));
+        const bool last = left[0] + left[1] == 0;
+        if (bits == 32) hipLaunchKernelGGL(k_adamw32, grid, dim3(256), 0, stream, tab, hp, st, last);
+        else hipLaunchKernelGGL(k_adamw8, grid, dim3(256), 0, stream, tab, hp, st, last);
+        tab.n = 0, tab.chunks = 0;
+    };
+    if (left[0] + left[1] == 0) hipLaunchKernelGGL(k_adamw_none, dim3(1), dim3(1), 0, stream, factor, st);
     for (int bits : {32, 8}) {
-        Table tab;
-        tab.n = 0, tab.first[0] = 0;
-        const auto flush = [&] {
-            if (tab.n == 0) return;
-            const dim3 grid(unsigned(tab.first[tab.n]));
-            if (bits == 32) hipLaunchKernelGGL(k_adamw32, grid, dim3(256), 0, stream, tab, hp, ctl);
-            else hipLaunchKernelGGL(k_adamw8, grid, dim3(256), 0, stream, tab, hp, ctl);
-            tab.n = 0;
-        };
         for (int i = 0; i < count; ++i) {
             if (q[i].state_bits != bits || q[i].numel == 0) continue;
-            const int64_t ch = (q[i].numel + 1023) / 1024;
-            if (tab.n == kMaxEntries || (tab.n && tab.first[tab.n] + ch > (int64_t(1) << 30))) flush();
+            const int64_t ch = chunks_of(q[i]);
+            if (tab.n && full(tab, kMaxEntries, ch)) flush(bits);
             uint32_t flags = grad_flags(q[i]);
             const size_t am = bits == 32 ? 16 : 4;
             if (!aligned(q[i].param, 16) || !aligned(q[i].m, am) || !aligned(q[i].v, am) || !aligned(q[i].copy, 8))
                 flags &= ~uint32_t(kWide);
-            tab.e[tab.n] = Entry{q[i].param, q[i].grad, static_cast<uint16_t*>(q[i].copy), q[i].m, q[i].v,
-                                 static_cast<float2*>(static_cast<void*>(q[i].scale)), q[i].numel, q[i].weight_decay, flags};
-            tab.first[tab.n + 1] = tab.first[tab.n] + int32_t(ch);
-            ++tab.n;
+            tab.e[tab.n++] = Entry{q[i].param, q[i].grad, static_cast<uint16_t*>(q[i].copy), q[i].m, q[i].v,
+                                   static_cast<float2*>(static_cast<void*>(q[i].scale)), uint32_t(q[i].numel),
+                                   q[i].weight_decay, tab.chunks, flags};
+            tab.chunks += int32_t(ch);
+            --left[bits == 8];
         }
-        flush();
+        if (tab.n) flush(bits);
     }
     return hipGetLastError();
 }

@@ -268,7 +268,7 @@ def test_clip_and_mixed_list():
     v = [z(k, torch.uint8 if b == 8 else torch.float32) for k, b in zip(sizes, bits)]
     s = [z((-(-k // 256), 2), torch.float32) if b == 8 else None for k, b in zip(sizes, bits)]
     plist = B.ParamList(p, g, m, v, s, weight_decay=[0.1, 0.0, 0.0])
-    out, state = z(2, torch.float32), z(8, torch.int64)
+    out, state = z(2, torch.float32), z(B.ADAMW_STATE_BYTES // 8, torch.int64)
     lr = torch.tensor([0.02], device="cuda")
     B.grad_norm(plist, out, max_norm=2.0)
     B.adamw_step(plist, state, lr, factor=out[1:])
