@@ -293,10 +293,13 @@ typedef enum { PSC_NCHW = 0, PSC_NHWC = 1 } psc_layout;
 typedef enum { PSC_ACT_NONE = 0, PSC_ACT_RELU = 1, PSC_ACT_SILU = 2 } psc_act;
 
 /* Bytes of workspace of the forward (backward == 0) or backward call of these
- * sizes (0 is a valid answer); 256-byte aligned, it holds nothing from one
- * call to the next, and calls that may overlap need one each. */
+ * sizes (0 is a valid answer; fewer, often, where aligned != 0 says that every
+ * activation tensor begins at a multiple of 16 bytes); 256-byte aligned, it
+ * holds nothing from one call to the next, and calls that may overlap need one
+ * each. */
 psc_status psc_group_norm_workspace(int32_t dtype, int32_t layout, int32_t n, int32_t c, int32_t h,
-                                    int32_t w, int32_t groups, int32_t backward, size_t *bytes);
+                                    int32_t w, int32_t groups, int32_t backward, int32_t aligned,
+                                    size_t *bytes);
 
 /* d_y = act(u).  d_gamma and d_beta [c] may be NULL (1 and 0).  d_mean and
  * d_rstd [n][groups] receive the statistics that the backward reads; both may

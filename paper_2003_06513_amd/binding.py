@@ -129,7 +129,7 @@ def lib() -> ctypes.CDLL:
         "psc_dense3x3_fwd_workspace": ([i32, i32, i32, ctypes.POINTER(sz)], ctypes.c_int),
         "psc_dense3x3_fwd_ws": ([i32, P, i32, i32, i32, i32, P, i32, P, i32, P, P, sz, P], ctypes.c_int),
         "psc_maxpool2x2": ([i32, P, i32, i32, i32, i32, P, P], ctypes.c_int),
-        "psc_group_norm_workspace": ([i32] * 8 + [ctypes.POINTER(sz)], ctypes.c_int),
+        "psc_group_norm_workspace": ([i32] * 9 + [ctypes.POINTER(sz)], ctypes.c_int),
         "psc_group_norm_fwd": ([i32, i32, P] + [i32] * 5 + [P, P, ctypes.c_float, i32, P, P, P, P, sz, P], ctypes.c_int),
         "psc_group_norm_bwd": ([i32, i32, P, P] + [i32] * 5 + [P, P, P, P, i32, P, P, P, P, sz, P], ctypes.c_int),
         "psc_grad_norm": ([P, i32, ctypes.c_float, ctypes.c_float, P, P, sz, P], ctypes.c_int),
@@ -672,11 +672,12 @@ def _act_code(act) -> int:
 
 
 def group_norm_workspace(dtype: int, layout: int, n: int, c: int, h: int, w: int, groups: int,
-                         backward: bool = False) -> int:
+                         backward: bool = False, aligned: bool = False) -> int:
     """psc_group_norm_workspace: bytes of scratch (host only)."""
     b = ctypes.c_size_t(0)
     _check(lib().psc_group_norm_workspace(int(dtype), int(layout), int(n), int(c), int(h), int(w), int(groups),
-                                          int(bool(backward)), ctypes.byref(b)), "psc_group_norm_workspace")
+                                          int(bool(backward)), int(bool(aligned)), ctypes.byref(b)),
+           "psc_group_norm_workspace")
     return int(b.value)
 
 
@@ -712,9 +713,10 @@ def group_norm_fwd(x, groups: int, gamma, beta, y, eps: float = 1e-5, act: str =
     n, c, h, w = x.shape
     groups = int(groups)
     _same_device(x)
-    wp, wb, ws = _norm_scratch(ws, stream, dt, layout, n, c, h, w, groups, False)
-    _check(lib().psc_group_norm_fwd(dt, layout, x.data_ptr() or None, n, c, h, w, groups, _vector(gamma, c, x, "gamma"),
-                                    _vector(beta, c, x, "beta"), eps, _act_code(act), _like(y, x, layout, "y"),
+    xp, yp = x.data_ptr(), _like(y, x, layout, "y") or 0
+    wp, wb, ws = _norm_scratch(ws, stream, dt, layout, n, c, h, w, groups, False, not (xp | yp) & 15)
+    _check(lib().psc_group_norm_fwd(dt, layout, xp, n, c, h, w, groups, _vector(gamma, c, x, "gamma"),
+                                    _vector(beta, c, x, "beta"), eps, _act_code(act), yp,
                                     _vector(mean, n * groups, x, "mean"), _vector(rstd, n * groups, x, "rstd"), wp, wb,
                                     _stream(stream)), "psc_group_norm_fwd")
 
@@ -728,12 +730,13 @@ def group_norm_bwd(x, dy, groups: int, gamma, beta, mean, rstd, dx, dgamma=None,
     n, c, h, w = x.shape
     groups = int(groups)
     _same_device(x)
-    wp, wb, ws = _norm_scratch(ws, stream, dt, layout, n, c, h, w, groups, True)
-    _check(lib().psc_group_norm_bwd(dt, layout, x.data_ptr() or None, _like(dy, x, layout, "dy"), n, c, h, w, groups,
-                                    _vector(gamma, c, x, "gamma"), _vector(beta, c, x, "beta"),
-                                    _vector(mean, n * groups, x, "mean"), _vector(rstd, n * groups, x, "rstd"),
-                                    _act_code(act), _like(dx, x, layout, "dx"), _vector(dgamma, c, x, "dgamma"),
-                                    _vector(dbeta, c, x, "dbeta"), wp, wb, _stream(stream)), "psc_group_norm_bwd")
+    xp, gp, dp = x.data_ptr(), _like(dy, x, layout, "dy") or 0, _like(dx, x, layout, "dx") or 0
+    wp, wb, ws = _norm_scratch(ws, stream, dt, layout, n, c, h, w, groups, True, not (xp | gp | dp) & 15)
+    _check(lib().psc_group_norm_bwd(dt, layout, xp, gp, n, c, h, w, groups, _vector(gamma, c, x, "gamma"),
+                                    _vector(beta, c, x, "beta"), _vector(mean, n * groups, x, "mean"),
+                                    _vector(rstd, n * groups, x, "rstd"), _act_code(act), dp,
+                                    _vector(dgamma, c, x, "dgamma"), _vector(dbeta, c, x, "dbeta"), wp, wb,
+                                    _stream(stream)), "psc_group_norm_bwd")
 
 
 # ------------------------------------------------------------------ the optimiser

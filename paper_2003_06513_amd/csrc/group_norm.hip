@@ -174,16 +174,20 @@ Plan plan_of(const GroupNormArgs& a, bool backward, int vec) {
     return a.channels_last ? plan_cols(a, backward, vec) : plan_rows(a, backward, vec);
 }
 
-// How the tensors lie: all alike to the bytes of a vector, and rows (pixels) of whole vectors.
-int vec_of(const GroupNormArgs& a, bool backward, const void* x, const void* y, const void* z) {
-    const bool columns_back = a.channels_last && backward;
-    const int v = vector_of(a.dtype, columns_back);
-    const uintptr_t mask = uintptr_t(v) * (a.dtype == DT_F16 ? 2 : 4) - 1, at = reinterpret_cast<uintptr_t>(x) & mask;
-    for (const void* p : {y, z})
-        if (p && (reinterpret_cast<uintptr_t>(p) & mask) != at) return 0;
-    const int64_t row = a.channels_last ? a.c : int64_t(a.h) * a.w;
-    if (at == 0 && row % v == 0) return 1;
+// How the tensors lie, by their offset from a multiple of 16 bytes (-1: not
+// all alike): rows (pixels) of whole vectors, rows that begin anywhere, or
+// single elements.
+int vec_of(const GroupNormArgs& a, bool backward, int offset) {
+    const int v = vector_of(a.dtype, a.channels_last && backward);
+    if (offset < 0) return 0;
+    if (offset % (v * (a.dtype == DT_F16 ? 2 : 4)) == 0 && (a.channels_last ? a.c : int64_t(a.h) * a.w) % v == 0) return 1;
     return a.channels_last ? 0 : 2;
+}
+int offset_of(const void* x, const void* y, const void* z) {
+    const uintptr_t at = reinterpret_cast<uintptr_t>(x) & 15u;
+    for (const void* p : {y, z})
+        if (p && (reinterpret_cast<uintptr_t>(p) & 15u) != at) return -1;
+    return int(at);
 }
 
 size_t bytes_of(const GroupNormArgs& a, bool backward, int vec) {
@@ -206,8 +210,9 @@ void combine_bwd(const float2* parts, int64_t groups, int per_group, int pieces,
 
 }  // namespace gn
 
-// What the call may need however its tensors lie.
-size_t group_norm_workspace_bytes(const GroupNormArgs& a, bool backward) {
+// What the call may need however its tensors lie, or if they are aligned.
+size_t group_norm_workspace_bytes(const GroupNormArgs& a, bool backward, bool aligned) {
+    if (aligned) return gn::bytes_of(a, backward, gn::vec_of(a, backward, 0));
     size_t most = 0;
     for (int vec : {0, 1, 2}) {
         const size_t b = gn::bytes_of(a, backward, vec);
@@ -219,7 +224,8 @@ size_t group_norm_workspace_bytes(const GroupNormArgs& a, bool backward) {
 hipError_t launch_group_norm_fwd(const GroupNormArgs& a, const void* x, const float* gamma, const float* beta, float eps,
                                  void* y, float* mean, float* rstd, void* ws, hipStream_t stream) {
     using namespace gn;
-    Plan p = plan_of(a, false, vec_of(a, false, x, y, nullptr));
+    const int offset = offset_of(x, y, nullptr);
+    Plan p = plan_of(a, false, vec_of(a, false, offset));
     const Params q{gamma, beta, a.act};
     float4* parts = static_cast<float4*>(ws);
     const int64_t rows = int64_t(a.n) * a.c * p.pieces, groups = int64_t(a.n) * a.groups;
@@ -231,7 +237,7 @@ hipError_t launch_group_norm_fwd(const GroupNormArgs& a, const void* x, const fl
         if (a.dtype == DT_F16) cols_fwd<DT_F16>(p, a.n, x, q, eps, y, mean, rstd, parts, stream);
         else cols_fwd<DT_F32>(p, a.n, x, q, eps, y, mean, rstd, parts, stream);
     } else {
-        p.rows.lead = int((reinterpret_cast<uintptr_t>(x) & 15u) / (a.dtype == DT_F16 ? 2 : 4));
+        p.rows.lead = offset < 0 ? 0 : offset / (a.dtype == DT_F16 ? 2 : 4);
         if (a.dtype == DT_F16) rows_fwd<DT_F16>(p, rows, x, q, eps, y, mean, rstd, parts, stream);
         else rows_fwd<DT_F32>(p, rows, x, q, eps, y, mean, rstd, parts, stream);
     }
@@ -242,7 +248,8 @@ hipError_t launch_group_norm_bwd(const GroupNormArgs& a, const void* x, const vo
                                  const float* beta, const float* mean, const float* rstd, void* dx, float* dgamma,
                                  float* dbeta, void* ws, hipStream_t stream) {
     using namespace gn;
-    Plan p = plan_of(a, true, vec_of(a, true, x, dy, dx));
+    const int offset = offset_of(x, dy, dx);
+    Plan p = plan_of(a, true, vec_of(a, true, offset));
     const Params q{gamma, beta, a.act};
     float2* ab = static_cast<float2*>(ws);
     const int64_t rows = int64_t(a.n) * a.c * p.pieces;
@@ -259,7 +266,7 @@ hipError_t launch_group_norm_bwd(const GroupNormArgs& a, const void* x, const vo
             if (a.dtype == DT_F16) cols_bwd<DT_F16>(p, a.n, x, dy, q, mean, rstd, dx, sums, s12, tail, stream);
             else cols_bwd<DT_F32>(p, a.n, x, dy, q, mean, rstd, dx, sums, s12, tail, stream);
         } else {
-            p.rows.lead = int((reinterpret_cast<uintptr_t>(x) & 15u) / (a.dtype == DT_F16 ? 2 : 4));
+            p.rows.lead = offset < 0 ? 0 : offset / (a.dtype == DT_F16 ? 2 : 4);
             if (a.dtype == DT_F16) rows_bwd<DT_F16>(p, rows, x, dy, q, mean, rstd, dx, sums, s12, tail, stream);
             else rows_bwd<DT_F32>(p, rows, x, dy, q, mean, rstd, dx, sums, s12, tail, stream);
         }

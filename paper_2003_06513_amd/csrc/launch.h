@@ -152,7 +152,8 @@ struct GroupNormArgs {
     int n, c, h, w, groups;
     int act;
 };
-size_t group_norm_workspace_bytes(const GroupNormArgs& a, bool backward);
+// aligned: every activation tensor begins at a multiple of 16 bytes.
+size_t group_norm_workspace_bytes(const GroupNormArgs& a, bool backward, bool aligned);
 hipError_t launch_group_norm_fwd(const GroupNormArgs& a, const void* x, const float* gamma, const float* beta, float eps,
                                  void* y, float* mean, float* rstd, void* ws, hipStream_t stream);
 hipError_t launch_group_norm_bwd(const GroupNormArgs& a, const void* x, const void* dy, const float* gamma,

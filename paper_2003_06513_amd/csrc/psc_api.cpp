@@ -576,11 +576,11 @@ static psc_status check_ws(const char* what, size_t need, const void* d_ws, size
 }
 
 psc_status psc_group_norm_workspace(int32_t dtype, int32_t layout, int32_t n, int32_t c, int32_t h, int32_t w,
-                                    int32_t groups, int32_t backward, size_t* bytes) {
+                                    int32_t groups, int32_t backward, int32_t aligned, size_t* bytes) {
     psc::GroupNormArgs a;
     if (psc_status s = check_group_norm(dtype, layout, n, c, h, w, groups, PSC_ACT_NONE, &a)) return s;
     if (!bytes) return fail(PSC_ERR_ARG, "bytes is NULL");
-    *bytes = psc::group_norm_workspace_bytes(a, backward != 0);
+    *bytes = psc::group_norm_workspace_bytes(a, backward != 0, aligned != 0);
     return ok();
 }
 
@@ -596,7 +596,10 @@ psc_status psc_group_norm_fwd(int32_t dtype, int32_t layout, const void* d_x, in
     if (!d_x || !d_y) return fail(PSC_ERR_ARG, "d_x and d_y must be non-NULL");
     const size_t bytes = size_t(int64_t(n) * c * h * w) * elt_size(dtype);
     if (overlaps(d_x, bytes, d_y, bytes)) return fail(PSC_ERR_ARG, "d_y overlaps d_x");
-    if (psc_status s = check_ws("psc_group_norm_fwd", psc::group_norm_workspace_bytes(a, false), d_ws, ws_bytes))
+    const uintptr_t bits = reinterpret_cast<uintptr_t>(d_x) | reinterpret_cast<uintptr_t>(d_y);
+    if (bits & (elt_size(dtype) - 1)) return fail(PSC_ERR_ARG, "d_x or d_y is not aligned to its elements");
+    if (psc_status s = check_ws("psc_group_norm_fwd", psc::group_norm_workspace_bytes(a, false, (bits & 15u) == 0), d_ws,
+                                ws_bytes))
         return s;
     return device_status(psc::launch_group_norm_fwd(a, d_x, d_gamma, d_beta, eps, d_y, d_mean, d_rstd, d_ws,
                                                     as_stream(stream)),
@@ -614,7 +617,10 @@ psc_status psc_group_norm_bwd(int32_t dtype, int32_t layout, const void* d_x, co
     const size_t bytes = size_t(int64_t(n) * c * h * w) * elt_size(dtype);
     if (overlaps(d_x, bytes, d_dx, bytes) || overlaps(d_dy, bytes, d_dx, bytes))
         return fail(PSC_ERR_ARG, "d_dx overlaps d_x or d_dy");
-    if (psc_status s = check_ws("psc_group_norm_bwd", psc::group_norm_workspace_bytes(a, true), d_ws, ws_bytes))
+    const uintptr_t bits = reinterpret_cast<uintptr_t>(d_x) | reinterpret_cast<uintptr_t>(d_dy) | reinterpret_cast<uintptr_t>(d_dx);
+    if (bits & (elt_size(dtype) - 1)) return fail(PSC_ERR_ARG, "d_x, d_dy or d_dx is not aligned to its elements");
+    if (psc_status s = check_ws("psc_group_norm_bwd", psc::group_norm_workspace_bytes(a, true, (bits & 15u) == 0), d_ws,
+                                ws_bytes))
         return s;
     return device_status(psc::launch_group_norm_bwd(a, d_x, d_dy, d_gamma, d_beta, d_mean, d_rstd, d_dx, d_dgamma,
                                                     d_dbeta, d_ws, as_stream(stream)),

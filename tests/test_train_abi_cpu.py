@@ -8,7 +8,7 @@ import torch
 
 from paper_2003_06513_amd import binding as B
 
-FAKE, FAR = 0x10000, 0x40000000       # never dereferenced
+FAKE, FAR = 0x10000, 0x400000000       # never dereferenced
 
 
 @pytest.fixture(scope="module")
@@ -29,7 +29,7 @@ SHARED = [
     (dict(c=0), "shape"), (dict(h=0), "shape"), (dict(w=32769), "shape"), (dict(groups=0), "groups"),
     (dict(groups=4), "groups"), (dict(groups=12), "groups"), (dict(act=3), "act"), (dict(act=-1), "act"),
     (dict(n=60000, c=60000, groups=1), "2^31-1"), (dict(n=60000, c=1, h=32768, w=32768, groups=1), "2^31-1"),
-    (dict(x=None), "non-NULL"),
+    (dict(x=None), "non-NULL"), (dict(x=FAKE + 2), "aligned"),
 ]
 
 
@@ -53,17 +53,18 @@ def test_backward_refuses(L, change, text):
 def test_group_norm_workspace(L):
     big = dict(c=64, h=56, w=56, groups=2)
     need = B.group_norm_workspace(0, 0, 2, 64, 56, 56, 2, True)
-    assert need > 0
+    assert need >= B.group_norm_workspace(0, 0, 2, 64, 56, 56, 2, True, aligned=True) > 0
+    need = B.group_norm_workspace(0, 0, 2, 64, 56, 56, 2, True, aligned=True)
     for ws, size in ((None, need), (FAKE, need - 1), (FAKE + 8, need)):
         assert L.psc_group_norm_bwd(*{**BWD, **big, "ws": ws, "ws_bytes": size}.values()) == B.PSC_ERR_WORKSPACE
-    need = B.group_norm_workspace(0, 0, 1, 8, 300, 300, 1)
+    need = B.group_norm_workspace(0, 0, 1, 8, 300, 300, 1, aligned=True)
     if need:
         args = {**FWD, "n": 1, "c": 8, "h": 300, "w": 300, "groups": 1, "ws": FAKE, "ws_bytes": need - 1}
         assert L.psc_group_norm_fwd(*args.values()) == B.PSC_ERR_WORKSPACE
     assert B.group_norm_workspace(0, 0, 0, 64, 56, 56, 2, True) >= 0
     out = ctypes.c_size_t(0)
-    _says(L.psc_group_norm_workspace(0, 0, 1, 6, 4, 4, 5, 0, ctypes.byref(out)), B.PSC_ERR_ARG, "groups")
-    _says(L.psc_group_norm_workspace(0, 0, 1, 6, 4, 4, 3, 0, None), B.PSC_ERR_ARG, "NULL")
+    _says(L.psc_group_norm_workspace(0, 0, 1, 6, 4, 4, 5, 0, 0, ctypes.byref(out)), B.PSC_ERR_ARG, "groups")
+    _says(L.psc_group_norm_workspace(0, 0, 1, 6, 4, 4, 3, 0, 0, None), B.PSC_ERR_ARG, "NULL")
     # no images: nothing to do, whatever the pointers are
     assert L.psc_group_norm_fwd(*{**FWD, "n": 0, "x": None, "y": None, "ws": None}.values()) == B.PSC_OK
 
