@@ -291,6 +291,10 @@ template <int V, bool MASK> struct Base {
     __device__ __forceinline__ Base(const Rows& s, int64_t first) {
         phase = MASK ? int((first + s.lead) & (V - 1)) : 0;
         at = first - phase;
+        shift(s, 0);
+    }
+    __device__ __forceinline__ void shift(const Rows& s, int64_t by) {
+        at += by;
         lo = at < 0 ? int(-at) : 0;
         const int64_t left = s.total - at;
         hi = left < (1 << 30) ? int(left) : 1 << 30;

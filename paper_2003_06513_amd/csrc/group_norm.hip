@@ -221,25 +221,60 @@ size_t group_norm_workspace_bytes(const GroupNormArgs& a, bool backward, bool al
     return most;
 }
 
+namespace {
+using namespace gn;
+
+// The images of a launch: a launch has fewer than 2^32 threads, which groups of
+// one value pass before their tensor does its limit.  A multiple of 16, so
+// that every launch's tensors lie as the first's.
+int images_of(const GroupNormArgs& a, const Plan& p) {
+    const int64_t blocks = !a.channels_last ? (p.held ? a.groups : ceil_div(int64_t(a.c) * p.pieces, 4) + 1)
+                                            : int64_t(p.cols.tiles + p.cols.near) * p.cols.chunks;
+    const int64_t threads = (blocks > a.groups ? blocks : a.groups) * (p.threads > 256 ? p.threads : 256);
+    const int64_t most = (int64_t(1) << 31) / threads / 16 * 16;
+    return a.n <= most ? a.n : int(most < 16 ? 16 : most);
+}
+// The plan of some of the images.
+Plan part_of(const GroupNormArgs& a, Plan p, int n) {
+    p.grid = a.channels_last ? cols_grid(p.cols, n, a.dtype == DT_F16 ? 2 : 4) : int64_t(n) * a.groups;
+    p.rows.total = int64_t(n) * a.c * a.h * a.w;
+    return p;
+}
+const void* at(const void* p, int64_t elements, int dtype) {
+    return static_cast<const char*>(p) + elements * (dtype == DT_F16 ? 2 : 4);
+}
+void* at(void* p, int64_t elements, int dtype) { return static_cast<char*>(p) + elements * (dtype == DT_F16 ? 2 : 4); }
+
+}  // namespace
+
 hipError_t launch_group_norm_fwd(const GroupNormArgs& a, const void* x, const float* gamma, const float* beta, float eps,
                                  void* y, float* mean, float* rstd, void* ws, hipStream_t stream) {
-    using namespace gn;
     const int offset = offset_of(x, y, nullptr);
-    Plan p = plan_of(a, false, vec_of(a, false, offset));
+    Plan whole = plan_of(a, false, vec_of(a, false, offset));
+    whole.rows.lead = offset < 0 ? 0 : offset / (a.dtype == DT_F16 ? 2 : 4);
     const Params q{gamma, beta, a.act};
-    float4* parts = static_cast<float4*>(ws);
-    const int64_t rows = int64_t(a.n) * a.c * p.pieces, groups = int64_t(a.n) * a.groups;
-    if (!p.held && !p.joined && !mean) {
-        mean = static_cast<float*>(static_cast<void*>(parts + rows));
-        rstd = mean + groups;
+    float4* all = static_cast<float4*>(ws);
+    const int64_t image = int64_t(a.c) * a.h * a.w, rows = int64_t(a.c) * whole.pieces;
+    if (!whole.held && !whole.joined && !mean) {
+        mean = static_cast<float*>(static_cast<void*>(all + a.n * rows));
+        rstd = mean + int64_t(a.n) * a.groups;
     }
-    if (a.channels_last) {
-        if (a.dtype == DT_F16) cols_fwd<DT_F16>(p, a.n, x, q, eps, y, mean, rstd, parts, stream);
-        else cols_fwd<DT_F32>(p, a.n, x, q, eps, y, mean, rstd, parts, stream);
-    } else {
-        p.rows.lead = offset < 0 ? 0 : offset / (a.dtype == DT_F16 ? 2 : 4);
-        if (a.dtype == DT_F16) rows_fwd<DT_F16>(p, rows, x, q, eps, y, mean, rstd, parts, stream);
-        else rows_fwd<DT_F32>(p, rows, x, q, eps, y, mean, rstd, parts, stream);
+    const int most = images_of(a, whole);
+    for (int first = 0; first < a.n; first += most) {
+        const int n = a.n - first < most ? a.n - first : most;
+        const Plan p = part_of(a, whole, n);
+        const void* xn = at(x, first * image, a.dtype);
+        void* yn = at(y, first * image, a.dtype);
+        float* mn = mean ? mean + int64_t(first) * a.groups : nullptr;
+        float* rn = mean ? rstd + int64_t(first) * a.groups : nullptr;
+        float4* parts = all + first * rows;
+        if (a.channels_last) {
+            if (a.dtype == DT_F16) cols_fwd<DT_F16>(p, n, xn, q, eps, yn, mn, rn, parts, stream);
+            else cols_fwd<DT_F32>(p, n, xn, q, eps, yn, mn, rn, parts, stream);
+        } else {
+            if (a.dtype == DT_F16) rows_fwd<DT_F16>(p, n * rows, xn, q, eps, yn, mn, rn, parts, stream);
+            else rows_fwd<DT_F32>(p, n * rows, xn, q, eps, yn, mn, rn, parts, stream);
+        }
     }
     return hipGetLastError();
 }
@@ -247,32 +282,39 @@ hipError_t launch_group_norm_fwd(const GroupNormArgs& a, const void* x, const fl
 hipError_t launch_group_norm_bwd(const GroupNormArgs& a, const void* x, const void* dy, const float* gamma,
                                  const float* beta, const float* mean, const float* rstd, void* dx, float* dgamma,
                                  float* dbeta, void* ws, hipStream_t stream) {
-    using namespace gn;
     const int offset = offset_of(x, dy, dx);
-    Plan p = plan_of(a, true, vec_of(a, true, offset));
+    Plan whole = plan_of(a, true, vec_of(a, true, offset));
+    whole.rows.lead = offset < 0 ? 0 : offset / (a.dtype == DT_F16 ? 2 : 4);
     const Params q{gamma, beta, a.act};
-    float2* ab = static_cast<float2*>(ws);
-    const int64_t rows = int64_t(a.n) * a.c * p.pieces;
-    float2* s12 = ab + rows;
-    Tail tail{ab, a.n, a.c, p.pieces, dgamma, dbeta, 0};
-    const unsigned last = tail_blocks(tail);
+    const int64_t image = int64_t(a.c) * a.h * a.w, rows = int64_t(a.c) * whole.pieces;
+    float2* all = static_cast<float2*>(ws);
+    float2* s12 = all + a.n * rows;
+    const Tail wanted{all, a.n, a.c, whole.pieces, dgamma, dbeta, 0};
+    const unsigned last = tail_blocks(wanted);
     // a held batch of one image: the sums of its channels are the gradients
-    const bool once = p.held && a.n == 1;
-    Sums sums{ab, nullptr, nullptr};
-    if (p.held && (once || !last)) sums.ab = nullptr;
-    if (once) sums.dgamma = dgamma, sums.dbeta = dbeta;
-    if (a.n > 0) {
+    const bool once = whole.held && a.n == 1;
+    const int most = images_of(a, whole);
+    for (int first = 0; first < a.n; first += most) {
+        const int n = a.n - first < most ? a.n - first : most;
+        const Plan p = part_of(a, whole, n);
+        const void *xn = at(x, first * image, a.dtype), *gn = at(dy, first * image, a.dtype);
+        void* dn = at(dx, first * image, a.dtype);
+        const float *mn = mean + int64_t(first) * a.groups, *rn = rstd + int64_t(first) * a.groups;
+        Sums sums{whole.held && (once || !last) ? nullptr : all + first * rows, once ? dgamma : nullptr,
+                  once ? dbeta : nullptr};
+        float2* sn = s12 + int64_t(first) * a.groups;
+        Tail tail = wanted;         // behind the last images' pieces
+        if (first + n < a.n) tail.dgamma = tail.dbeta = nullptr;
         if (a.channels_last) {
-            if (a.dtype == DT_F16) cols_bwd<DT_F16>(p, a.n, x, dy, q, mean, rstd, dx, sums, s12, tail, stream);
-            else cols_bwd<DT_F32>(p, a.n, x, dy, q, mean, rstd, dx, sums, s12, tail, stream);
+            if (a.dtype == DT_F16) cols_bwd<DT_F16>(p, n, xn, gn, q, mn, rn, dn, sums, sn, tail, stream);
+            else cols_bwd<DT_F32>(p, n, xn, gn, q, mn, rn, dn, sums, sn, tail, stream);
         } else {
-            p.rows.lead = offset < 0 ? 0 : offset / (a.dtype == DT_F16 ? 2 : 4);
-            if (a.dtype == DT_F16) rows_bwd<DT_F16>(p, rows, x, dy, q, mean, rstd, dx, sums, s12, tail, stream);
-            else rows_bwd<DT_F32>(p, rows, x, dy, q, mean, rstd, dx, sums, s12, tail, stream);
+            if (a.dtype == DT_F16) rows_bwd<DT_F16>(p, n * rows, xn, gn, q, mn, rn, dn, sums, sn, tail, stream);
+            else rows_bwd<DT_F32>(p, n * rows, xn, gn, q, mn, rn, dn, sums, sn, tail, stream);
         }
     }
-    if (last && !once && (p.held || a.n == 0))
-        hipLaunchKernelGGL(k_gn_param, dim3(last), dim3(1024), 0, stream, tail);
+    if (last && !once && (whole.held || a.n == 0))
+        hipLaunchKernelGGL(k_gn_param, dim3(last), dim3(1024), 0, stream, wanted);
     return hipGetLastError();
 }
 

@@ -181,15 +181,30 @@ __device__ __forceinline__ Piece this_piece(const Rows& s, int pieces) {
     p.c = int(p.row % unsigned(s.cg * s.groups));
     return p;
 }
-// Calls f(i, window, on): the vectors of a row from `skip` on, as above.
+// The base of a piece: its first vector, `skip` vectors behind the row's.  (From
+// there, a row of 2^30 elements has no offset of more than 32 bits.)
+template <int V, bool MASK> struct PieceBase : Base<V, MASK> {
+    bool first;         // the row begins in this piece
+    int left;           // elements from the base to the end of the row
+    __device__ __forceinline__ PieceBase(const Rows& s, int64_t row, int skip)
+        : Base<V, MASK>(s, row), first(skip == 0), left(this->phase + s.hw - skip * V) {
+        this->shift(s, int64_t(skip) * V);
+    }
+};
+// Calls f(i, window, on) for the vectors of a piece, as above.
 template <int V, bool MASK, int K, class F>
-__device__ __forceinline__ void each_of_piece(const Rows& s, const Base<V, MASK>& b, int skip, F f) {
+__device__ __forceinline__ void each_of_piece(const PieceBase<V, MASK>& b, F f) {
     const int lane = int(threadIdx.x & 63);
 #pragma unroll
     for (int i = 0; i < K; ++i) {
-        const int k = skip + i * 64 + lane;
-        const bool on = has<V, MASK>(b, 0, s.hw, k);
-        f(i, window<V, MASK>(b, 0, s.hw, on ? k : 0), on);
+        const int from = (i * 64 + lane) * V;
+        const bool on = from < b.left;
+        Window w;
+        w.from = on ? from : 0;
+        const int left = b.left - w.from;
+        w.lo = MASK && b.first && w.from == 0 ? b.phase : 0;
+        w.hi = !MASK || left >= V ? V : left;
+        f(i, w, on);
     }
 }
 
@@ -200,12 +215,11 @@ __global__ __launch_bounds__(256, 4) void k_gn_rowparts_fwd(const typename Elt<D
     using P = Pack<DT, V>;
     const Piece p = this_piece(s, pieces);
     if (p.id >= count) return;
-    const Base<V, MASK> b(s, int64_t(p.row) * s.hw);
-    const int skip = p.piece * K * 64;
+    const PieceBase<V, MASK> b(s, int64_t(p.row) * s.hw, p.piece * K * 64);
     typename P::R d[K];
-    each_of_piece<V, MASK, K>(s, b, skip, [&](int i, const Window& w, bool) { d[i] = load<DT, V, MASK>(x, b, w); });
+    each_of_piece<V, MASK, K>(b, [&](int i, const Window& w, bool) { d[i] = load<DT, V, MASK>(x, b, w); });
     float sum = 0.f, num = 0.f;
-    each_of_piece<V, MASK, K>(s, b, skip, [&](int i, const Window& w, bool on) {
+    each_of_piece<V, MASK, K>(b, [&](int i, const Window& w, bool on) {
         float f[V], t = 0.f;
         P::open(d[i], f);
         num += on ? float(w.hi - w.lo) : 0.f;
@@ -216,7 +230,7 @@ __global__ __launch_bounds__(256, 4) void k_gn_rowparts_fwd(const typename Elt<D
     num = wave_sum(num);
     const float mu = num > 0.f ? wave_sum(sum) / num : 0.f;
     float sq = 0.f;
-    each_of_piece<V, MASK, K>(s, b, skip, [&](int i, const Window& w, bool on) {
+    each_of_piece<V, MASK, K>(b, [&](int i, const Window& w, bool on) {
         float f[V], t = 0.f;
         P::open(d[i], f);
 #pragma unroll
@@ -243,10 +257,9 @@ __global__ __launch_bounds__(256, 4) void k_gn_rowwrite_fwd(const typename Elt<D
     using P = Pack<DT, V>;
     const Piece p = this_piece(s, pieces);
     if (p.id >= count) return;
-    const Base<V, MASK> b(s, int64_t(p.row) * s.hw);
-    const int skip = p.piece * K * 64;
+    const PieceBase<V, MASK> b(s, int64_t(p.row) * s.hw, p.piece * K * 64);
     typename P::R d[K];
-    each_of_piece<V, MASK, K>(s, b, skip, [&](int i, const Window& w, bool) { d[i] = load<DT, V, MASK>(x, b, w); });
+    each_of_piece<V, MASK, K>(b, [&](int i, const Window& w, bool) { d[i] = load<DT, V, MASK>(x, b, w); });
     Coeff k{0.f, 0.f, or_one(q.gamma, p.c), or_zero(q.beta, p.c)};
     if (parts) {
         const int per = s.cg * pieces;
@@ -256,7 +269,7 @@ __global__ __launch_bounds__(256, 4) void k_gn_rowwrite_fwd(const typename Elt<D
     } else {
         k.mu = mean[p.ng], k.r = rstd[p.ng];
     }
-    each_of_piece<V, MASK, K>(s, b, skip, [&](int i, const Window& w, bool on) {
+    each_of_piece<V, MASK, K>(b, [&](int i, const Window& w, bool on) {
         float f[V];
         P::open(d[i], f);
 #pragma unroll
@@ -266,23 +279,22 @@ __global__ __launch_bounds__(256, 4) void k_gn_rowwrite_fwd(const typename Elt<D
 }
 
 template <int DT, int V, bool MASK, int K, int ACT>
-__global__ __launch_bounds__(256, 4) void k_gn_rowparts_bwd(const typename Elt<DT>::T* __restrict__ x,
+__global__ __launch_bounds__(256, MASK ? 3 : 4) void k_gn_rowparts_bwd(const typename Elt<DT>::T* __restrict__ x,
                                                          const typename Elt<DT>::T* __restrict__ dy, Rows s, Params q,
                                                          int pieces, unsigned count, const float* __restrict__ mean,
                                                          const float* __restrict__ rstd, float2* __restrict__ parts) {
     using P = Pack<DT, V>;
     const Piece p = this_piece(s, pieces);
     if (p.id >= count) return;
-    const Base<V, MASK> b(s, int64_t(p.row) * s.hw);
-    const int skip = p.piece * K * 64;
+    const PieceBase<V, MASK> b(s, int64_t(p.row) * s.hw, p.piece * K * 64);
     typename P::R d[K], e[K];
-    each_of_piece<V, MASK, K>(s, b, skip, [&](int i, const Window& w, bool) {
+    each_of_piece<V, MASK, K>(b, [&](int i, const Window& w, bool) {
         d[i] = load<DT, V, MASK>(x, b, w);
         e[i] = load<DT, V, MASK>(dy, b, w);
     });
     const Coeff k = coeff_of(p, q, mean, rstd);
     float sa = 0.f, sb = 0.f;
-    each_of_piece<V, MASK, K>(s, b, skip, [&](int i, const Window& w, bool on) {
+    each_of_piece<V, MASK, K>(b, [&](int i, const Window& w, bool on) {
         float f[V], g[V], ta = 0.f, tb = 0.f;
         P::open(d[i], f);
         P::open(e[i], g);
@@ -312,10 +324,9 @@ __global__ __launch_bounds__(256, 4) void k_gn_rowwrite_bwd(const typename Elt<D
     if (blockIdx.x >= tail.first) return param_block(tail);
     const Piece p = this_piece(s, pieces);
     if (p.id >= count) return;
-    const Base<V, MASK> b(s, int64_t(p.row) * s.hw);
-    const int skip = p.piece * K * 64;
+    const PieceBase<V, MASK> b(s, int64_t(p.row) * s.hw, p.piece * K * 64);
     typename P::R d[K], e[K];
-    each_of_piece<V, MASK, K>(s, b, skip, [&](int i, const Window& w, bool) {
+    each_of_piece<V, MASK, K>(b, [&](int i, const Window& w, bool) {
         d[i] = load<DT, V, MASK>(x, b, w);
         e[i] = load<DT, V, MASK>(dy, b, w);
     });
@@ -324,7 +335,7 @@ __global__ __launch_bounds__(256, 4) void k_gn_rowwrite_bwd(const typename Elt<D
     const float2 sum = parts ? joined_back(parts + int64_t(p.ng) * per, per, pieces, q.gamma ? q.gamma + p.c / s.cg * s.cg : nullptr,
                                            float(s.cg) * float(s.hw), int(threadIdx.x & 63), 64)
                              : s12[p.ng];
-    each_of_piece<V, MASK, K>(s, b, skip, [&](int i, const Window& w, bool on) {
+    each_of_piece<V, MASK, K>(b, [&](int i, const Window& w, bool on) {
         float f[V], g[V];
         P::open(d[i], f);
         P::open(e[i], g);

@@ -433,8 +433,8 @@ uint32_t grad_flags(const ParamView& q) {
 size_t grad_norm_workspace_bytes() { return size_t(kNormBlocks) * sizeof(double); }
 
 namespace {
-// Tables are filled up to their room and to 2^30 chunks.
-template <class T> bool full(const T& tab, int room, int64_t more) { return tab.n == room || tab.chunks + more > (int64_t(1) << 30); }
+// Tables are filled up to their room and to 2^23 chunks (a launch has fewer than 2^32 threads).
+template <class T> bool full(const T& tab, int room, int64_t more) { return tab.n == room || tab.chunks + more > (int64_t(1) << 23); }
 template <class T> void clear(T& tab) {
     tab.n = 0, tab.chunks = 0;
     for (uint32_t& f : tab.first) f = ~0u;

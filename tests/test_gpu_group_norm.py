@@ -303,3 +303,65 @@ def test_graph_and_other_stream(shape, groups, layout):
         step(2 * tx, other)
     torch.cuda.synchronize()
     assert all(torch.equal(got[k], want[k]) for k in want)
+
+
+@pytest.mark.parametrize("layout", ["nchw", "nhwc"])
+def test_more_groups_than_a_launch_has_threads(layout):
+    """134 million groups of one value each: y = act(beta), dx = 0, dbeta = the sums of dy."""
+    torch = torch_mod()
+    n, c = 65535, 2048
+    fmt = torch.channels_last if layout == "nhwc" else torch.contiguous_format
+    note("group norm, 2^27 groups, %s" % layout)
+    x = torch.ones((n, c, 1, 2), dtype=torch.float16, device="cuda")[:, :, :, :1].contiguous(memory_format=fmt)
+    if layout == "nhwc":        # one pixel is in both layouts: two of them are not, with two values a group
+        x = torch.ones((n // 2, c, 1, 2), dtype=torch.float16, device="cuda").contiguous(memory_format=fmt)
+    n = x.shape[0]
+    y, beta = torch.zeros_like(x), torch.linspace(-1, 1, c, device="cuda")
+    mean, rstd = (torch.empty((n, c), device="cuda") for _ in range(2))
+    B.group_norm_fwd(x, c, None, beta, y, act="relu", mean=mean, rstd=rstd)
+    torch.cuda.synchronize()
+    want = beta.clamp(min=0).half().view(1, c, 1, 1)
+    assert bool((y == want).all()) and bool((mean == 1).all())
+    del mean
+    mean = torch.ones((n, c), device="cuda")
+    dgamma, dbeta = torch.empty(c, device="cuda"), torch.empty(c, device="cuda")
+    B.group_norm_bwd(x, x, c, None, beta, mean, rstd, y, dgamma, dbeta)
+    torch.cuda.synchronize()
+    assert not y.any() and not dgamma.any()
+    assert bool((dbeta == n * x.shape[3]).all())
+
+
+@pytest.mark.parametrize("shift", [0, 1])
+def test_row_of_four_gigabytes(shift):
+    """A channel of 2^30 values: offsets beyond 32 bits, aligned for wide accesses and not."""
+    torch = torch_mod()
+    side = 32768
+    buf = torch.empty(side * side + shift, device="cuda")
+    x = buf[shift:].view(1, 1, side, side)
+    x.normal_(3.0, 2.0)
+    out = torch.empty(side * side + shift, device="cuda")
+    y = out[shift:].view(1, 1, side, side)
+    mean, rstd = (torch.empty((1, 1), device="cuda") for _ in range(2))
+    note("group norm, 2^30 values, shift %d" % shift)
+    B.group_norm_fwd(x, 1, None, None, y, act="silu", mean=mean, rstd=rstd)
+    torch.cuda.synchronize()
+    rows = x.view(64, -1)
+    mu = sum(float(r.double().sum()) for r in rows) / x.numel()
+    var = sum(float((r.double() - mu).square().sum()) for r in rows) / x.numel()
+    # sums of 2^30 values by 2^20 partial ones: their roundings average out far below these
+    assert abs(float(mean) - mu) < 1e-5 and abs(float(rstd) * np.sqrt(var + 1e-5) - 1) < 1e-5
+    for r, o in zip(rows, y.view(64, -1)):
+        u = (r - mean.view(())) * rstd.view(())
+        assert float((o - u * torch.sigmoid(u)).abs().max()) < 1e-5
+    dx = torch.empty_like(out)[shift:].view(1, 1, side, side)
+    dbeta = torch.empty(1, device="cuda")
+    B.group_norm_bwd(x, y, 1, None, None, mean, rstd, dx, dbeta=dbeta)
+    torch.cuda.synchronize()
+    s1 = sum(float(o.double().sum()) for o in y.view(64, -1))
+    s2 = sum(float((o.double() * ((r - mean.view(())) * rstd.view(())).double()).sum())
+             for r, o in zip(rows, y.view(64, -1)))
+    assert abs(float(dbeta) / s1 - 1) < 1e-5
+    for r, o, d in zip(rows, y.view(64, -1), dx.view(64, -1)):
+        u = (r - mean.view(())) * rstd.view(())
+        want = rstd.view(()) * (o - s1 / x.numel() - u * (s2 / x.numel()))
+        assert float((d - want).abs().max()) < 1e-5
