@@ -58,9 +58,14 @@ template <int ACT> __device__ __forceinline__ float forward(const Coeff& k, floa
 template <int ACT> __device__ __forceinline__ float slope(const Coeff& k, float xh, float dy) {
     return act_back<ACT>(affine(xh, k.ga, k.be), dy);
 }
-template <int ACT> __device__ __forceinline__ float backward(const Coeff& k, float x, float dy, float s1, float s2) {
+// s: r gamma, r S1 / M and r S2 / M.
+struct Back {
+    float ga, s1, s2;
+};
+__device__ __forceinline__ Back back_of(const Coeff& k, float s1, float s2) { return Back{k.r * k.ga, k.r * s1, k.r * s2}; }
+template <int ACT> __device__ __forceinline__ float backward(const Coeff& k, const Back& s, float x, float dy) {
     const float xh = normal(k, x);
-    return k.r * (fmaf(k.ga, slope<ACT>(k, xh, dy), -s1) - xh * s2);
+    return fmaf(-s.s2, xh, fmaf(s.ga, slope<ACT>(k, xh, dy), -s.s1));
 }
 
 typedef uint32_t u4 __attribute__((ext_vector_type(4)));

@@ -209,14 +209,14 @@ __device__ __forceinline__ void sums_back(const typename Pack<DT, V>::R (&d)[K],
 }
 template <int DT, int V, int K, int ACT>
 __device__ __forceinline__ void write_back(const typename Pack<DT, V>::R (&d)[K], const typename Pack<DT, V>::R (&e)[K],
-                                           const Cols& q, const Place& p, const Coeff (&k)[V], const float (&s1)[V],
-                                           const float (&s2)[V], typename Elt<DT>::T* dxb) {
+                                           const Cols& q, const Place& p, const Coeff (&k)[V], const Back (&s)[V],
+                                           typename Elt<DT>::T* dxb) {
     each<DT, K>(q, p, [&](int i, uint32_t byte) {
         float f[V], g[V];
         Pack<DT, V>::open(d[i], f);
         Pack<DT, V>::open(e[i], g);
 #pragma unroll
-        for (int j = 0; j < V; ++j) f[j] = backward<ACT>(k[j], f[j], g[j], s1[j], s2[j]);
+        for (int j = 0; j < V; ++j) f[j] = backward<ACT>(k[j], s[j], f[j], g[j]);
         put(dxb, byte, Pack<DT, V>::close(f));
     });
 }
@@ -262,13 +262,13 @@ __global__ __launch_bounds__(threads_of(DT, V, K), 4) void k_gn_cols_bwd(const t
     each_group(q, count, ch, gamma, [&](int g, float sum) { gr[g] = sum / m; });
     each_group(q, count, ch2, gamma, [&](int g, float sum) { gr2[g] = sum / m; });
     __syncthreads();
+    Back s[V];
 #pragma unroll
     for (int j = 0; j < V; ++j) {
         const int g = p.on ? group_of(q, p.rel + j) : 0;
-        a[j] = gr[g];
-        b[j] = gr2[g];
+        s[j] = back_of(k[j], gr[g], gr2[g]);
     }
-    write_back<DT, V, K, ACT>(d, e, q, p, k, a, b, dx + at);
+    write_back<DT, V, K, ACT>(d, e, q, p, k, s, dx + at);
 }
 
 // ---- pieces: some pixels of some channels.
@@ -427,14 +427,14 @@ __global__ __launch_bounds__(256, 4) void k_gn_colwrite_bwd(const typename Elt<D
         });
         __syncthreads();
     }
-    float s1[V], s2[V];
+    Back s[V];
 #pragma unroll
     for (int j = 0; j < V; ++j) {
         const int c = p.on ? p.rel + j : 0;
         const float2 t = parts ? joined[group_of(q, c)] : s12[int64_t(p.n) * q.groups + group_of(q, p.c0 + c)];
-        s1[j] = t.x, s2[j] = t.y;
+        s[j] = back_of(k[j], t.x, t.y);
     }
-    write_back<DT, V, K, ACT>(d, e, q, p, k, s1, s2, dx + at);
+    write_back<DT, V, K, ACT>(d, e, q, p, k, s, dx + at);
 }
 
 // LDS of a block that joins its groups' pieces.

@@ -160,8 +160,9 @@ __global__ __launch_bounds__(threads_of(DT, V, K)) void k_gn_rows_bwd(const type
         float f[V], g[V];
         P::open(d[i], f);
         P::open(e[i], g);
+        const Back s = back_of(k, s1, s2);
 #pragma unroll
-        for (int j = 0; j < V; ++j) f[j] = backward<ACT>(k, f[j], g[j], s1, s2);
+        for (int j = 0; j < V; ++j) f[j] = backward<ACT>(k, s, f[j], g[j]);
         if (on) store<DT, V, MASK>(dx, b, w, f);
     }, Nothing());
 }
@@ -335,12 +336,13 @@ __global__ __launch_bounds__(256, 4) void k_gn_rowwrite_bwd(const typename Elt<D
     const float2 sum = parts ? joined_back(parts + int64_t(p.ng) * per, per, pieces, q.gamma ? q.gamma + p.c / s.cg * s.cg : nullptr,
                                            float(s.cg) * float(s.hw), int(threadIdx.x & 63), 64)
                              : s12[p.ng];
+    const Back back = back_of(k, sum.x, sum.y);
     each_of_piece<V, MASK, K>(b, [&](int i, const Window& w, bool on) {
         float f[V], g[V];
         P::open(d[i], f);
         P::open(e[i], g);
 #pragma unroll
-        for (int j = 0; j < V; ++j) f[j] = backward<ACT>(k, f[j], g[j], sum.x, sum.y);
+        for (int j = 0; j < V; ++j) f[j] = backward<ACT>(k, back, f[j], g[j]);
         if (on) store<DT, V, MASK>(dx, b, w, f);
     });
 }
