@@ -93,7 +93,7 @@ __device__ __forceinline__ void each_group(const Cols& q, int count, const float
     }
 }
 
-template <int DT, int V, int K, int ACT>
+template <int DT, int V, int K, int ACT, bool PAST>
 __global__ __launch_bounds__(threads_of(DT, V, K)) void k_gn_cols_fwd(const typename Elt<DT>::T* __restrict__ x, Cols q,
                                                                   int images, Params w, float eps,
                                                                   typename Elt<DT>::T* __restrict__ y,
@@ -110,7 +110,7 @@ __global__ __launch_bounds__(threads_of(DT, V, K)) void k_gn_cols_fwd(const type
     const int64_t at = base_of(q, p);
     const typename Elt<DT>::T* xb = x + at;
     typename P::R d[K];
-    each<DT, K>(q, p, [&](int i, uint32_t byte) { d[i] = get<typename P::R>(xb, byte); });
+    each<DT, K>(q, p, [&](int i, uint32_t byte) { d[i] = get<typename P::R, false>(xb, byte); });
     float ga[V], be[V];
     values<V>(w.gamma ? w.gamma + p.c0 + p.rel : nullptr, p.on, 1.f, ga);
     values<V>(w.beta ? w.beta + p.c0 + p.rel : nullptr, p.on, 0.f, be);
@@ -165,7 +165,7 @@ __global__ __launch_bounds__(threads_of(DT, V, K)) void k_gn_cols_fwd(const type
         P::open(d[i], f);
 #pragma unroll
         for (int j = 0; j < V; ++j) f[j] = forward<ACT>(Coeff{mu[j], r[j], ga[j], be[j]}, f[j]);
-        put(y + at, byte, P::close(f));
+        put<PAST>(y + at, byte, P::close(f));
     });
 }
 
@@ -207,7 +207,7 @@ __device__ __forceinline__ void sums_back(const typename Pack<DT, V>::R (&d)[K],
         }
     });
 }
-template <int DT, int V, int K, int ACT>
+template <int DT, int V, int K, int ACT, bool PAST>
 __device__ __forceinline__ void write_back(const typename Pack<DT, V>::R (&d)[K], const typename Pack<DT, V>::R (&e)[K],
                                            const Cols& q, const Place& p, const Coeff (&k)[V], const Back (&s)[V],
                                            typename Elt<DT>::T* dxb) {
@@ -217,11 +217,11 @@ __device__ __forceinline__ void write_back(const typename Pack<DT, V>::R (&d)[K]
         Pack<DT, V>::open(e[i], g);
 #pragma unroll
         for (int j = 0; j < V; ++j) f[j] = backward<ACT>(k[j], s[j], f[j], g[j]);
-        put(dxb, byte, Pack<DT, V>::close(f));
+        put<PAST>(dxb, byte, Pack<DT, V>::close(f));
     });
 }
 
-template <int DT, int V, int K, int ACT>
+template <int DT, int V, int K, int ACT, bool PAST>
 __global__ __launch_bounds__(threads_of(DT, V, K), 4) void k_gn_cols_bwd(const typename Elt<DT>::T* __restrict__ x,
                                                                      const typename Elt<DT>::T* __restrict__ dy, Cols q,
                                                                      int images, Params w,
@@ -240,8 +240,8 @@ __global__ __launch_bounds__(threads_of(DT, V, K), 4) void k_gn_cols_bwd(const t
     const typename Elt<DT>::T *xb = x + at, *gb = dy + at;
     typename P::R d[K], e[K];
     each<DT, K>(q, p, [&](int i, uint32_t byte) {
-        d[i] = get<typename P::R>(xb, byte);
-        e[i] = get<typename P::R>(gb, byte);
+        d[i] = get<typename P::R, PAST>(xb, byte);
+        e[i] = get<typename P::R, PAST>(gb, byte);
     });
     Coeff k[V];
     coefficients<V>(q, p, w, kept(q, p, mean, rstd), k);
@@ -268,7 +268,7 @@ __global__ __launch_bounds__(threads_of(DT, V, K), 4) void k_gn_cols_bwd(const t
         const int g = p.on ? group_of(q, p.rel + j) : 0;
         s[j] = back_of(k[j], gr[g], gr2[g]);
     }
-    write_back<DT, V, K, ACT>(d, e, q, p, k, s, dx + at);
+    write_back<DT, V, K, ACT, PAST>(d, e, q, p, k, s, dx + at);
 }
 
 // ---- pieces: some pixels of some channels.
@@ -285,7 +285,7 @@ __global__ __launch_bounds__(256, 4) void k_gn_colparts_fwd(const typename Elt<D
     const int64_t at = base_of(q, p);
     const typename Elt<DT>::T* xb = x + at;
     typename P::R d[K];
-    each<DT, K>(q, p, [&](int i, uint32_t byte) { d[i] = get<typename P::R>(xb, byte); });
+    each<DT, K>(q, p, [&](int i, uint32_t byte) { d[i] = get<typename P::R, false>(xb, byte); });
     float s[V], mu[V];
 #pragma unroll
     for (int j = 0; j < V; ++j) s[j] = 0.f;
@@ -327,7 +327,7 @@ template <class F> __device__ __forceinline__ void each_joined(const Cols& q, in
     for (int g = int(threadIdx.x) / q.join_lanes; g < count; g += int(blockDim.x) / q.join_lanes) f(g, lane);
 }
 
-template <int DT, int V, int K, int ACT>
+template <int DT, int V, int K, int ACT, bool PAST>
 __global__ __launch_bounds__(256, 4) void k_gn_colwrite_fwd(const typename Elt<DT>::T* __restrict__ x, Cols q, int images,
                                                             Params w, float* __restrict__ mean,
                                                             float* __restrict__ rstd,
@@ -340,7 +340,7 @@ __global__ __launch_bounds__(256, 4) void k_gn_colwrite_fwd(const typename Elt<D
     const int64_t at = base_of(q, p);
     const typename Elt<DT>::T* xb = x + at;
     typename P::R d[K];
-    each<DT, K>(q, p, [&](int i, uint32_t byte) { d[i] = get<typename P::R>(xb, byte); });
+    each<DT, K>(q, p, [&](int i, uint32_t byte) { d[i] = get<typename P::R, false>(xb, byte); });
     Coeff k[V];
     if (parts) {
         const int64_t first = int64_t(p.n) * q.c + p.c0, g0 = int64_t(p.n) * q.groups + group_of(q, p.c0);
@@ -362,7 +362,7 @@ __global__ __launch_bounds__(256, 4) void k_gn_colwrite_fwd(const typename Elt<D
         P::open(d[i], f);
 #pragma unroll
         for (int j = 0; j < V; ++j) f[j] = forward<ACT>(k[j], f[j]);
-        put(y + at, byte, P::close(f));
+        put<PAST>(y + at, byte, P::close(f));
     });
 }
 
@@ -380,8 +380,8 @@ __global__ __launch_bounds__(256, 4) void k_gn_colparts_bwd(const typename Elt<D
     const typename Elt<DT>::T *xb = x + at, *gb = dy + at;
     typename P::R d[K], e[K];
     each<DT, K>(q, p, [&](int i, uint32_t byte) {
-        d[i] = get<typename P::R>(xb, byte);
-        e[i] = get<typename P::R>(gb, byte);
+        d[i] = get<typename P::R, false>(xb, byte);
+        e[i] = get<typename P::R, false>(gb, byte);
     });
     Coeff k[V];
     coefficients<V>(q, p, w, kept(q, p, mean, rstd), k);
@@ -395,7 +395,7 @@ __global__ __launch_bounds__(256, 4) void k_gn_colparts_bwd(const typename Elt<D
             make_float2(sum_of_channel(lds, q, c), sum_of_channel(lds + all, q, c));
 }
 
-template <int DT, int V, int K, int ACT>
+template <int DT, int V, int K, int ACT, bool PAST>
 __global__ __launch_bounds__(256, 4) void k_gn_colwrite_bwd(const typename Elt<DT>::T* __restrict__ x,
                                                          const typename Elt<DT>::T* __restrict__ dy, Cols q, int images,
                                                          Params w, const float* __restrict__ mean,
@@ -411,8 +411,8 @@ __global__ __launch_bounds__(256, 4) void k_gn_colwrite_bwd(const typename Elt<D
     const typename Elt<DT>::T *xb = x + at, *gb = dy + at;
     typename P::R d[K], e[K];
     each<DT, K>(q, p, [&](int i, uint32_t byte) {
-        d[i] = get<typename P::R>(xb, byte);
-        e[i] = get<typename P::R>(gb, byte);
+        d[i] = get<typename P::R, false>(xb, byte);
+        e[i] = get<typename P::R, false>(gb, byte);
     });
     Coeff k[V];
     coefficients<V>(q, p, w, kept(q, p, mean, rstd), k);
@@ -434,11 +434,20 @@ __global__ __launch_bounds__(256, 4) void k_gn_colwrite_bwd(const typename Elt<D
         const float2 t = parts ? joined[group_of(q, c)] : s12[int64_t(p.n) * q.groups + group_of(q, p.c0 + c)];
         s[j] = back_of(k[j], t.x, t.y);
     }
-    write_back<DT, V, K, ACT>(d, e, q, p, k, s, dx + at);
+    write_back<DT, V, K, ACT, PAST>(d, e, q, p, k, s, dx + at);
 }
 
 // LDS of a block that joins its groups' pieces.
 unsigned joined_lds(const Plan& p) { return p.joined ? unsigned(sizeof(float2)) * unsigned(p.cols.tile / p.cols.cg) : 0u; }
+
+// Calls go with whether stores go past the caches: where they fill 64 bytes,
+// 128 in the backward, whose lanes write half as much (64 x 512 x 28 x 28 fp16
+// in tiles of 64 bytes 49 us, past the caches 52).
+template <int DT, int V, bool BACK, class F> void with_past(const Cols& q, F go) {
+    if constexpr (V > 1)
+        if (q.tile * int(sizeof(typename Elt<DT>::T)) >= (BACK ? 128 : 64)) return go(IntC<1>{});
+    go(IntC<0>{});
+}
 
 template <int DT, int V>
 void fwd(const Plan& p, int n, const void* x, const Params& q, float eps, void* y, float* mean, float* rstd, float4* parts,
@@ -447,22 +456,23 @@ void fwd(const Plan& p, int n, const void* x, const Params& q, float eps, void* 
     const T* xt = static_cast<const T*>(x);
     T* yt = static_cast<T*>(y);
     const dim3 grid(static_cast<unsigned>(p.grid)), block(static_cast<unsigned>(p.threads));
-    if (p.held) {
-        with_act(q.act, [&](auto act) {
-            with_count<DT, V, false>(p.k, [&](auto k) {
-                hipLaunchKernelGGL((k_gn_cols_fwd<DT, V, decltype(k)::value, decltype(act)::value>), grid, block,
-                                   cols_lds(p.cols, p.threads, 1, 2), st, xt, p.cols, n, q, eps, yt, mean, rstd);
-            });
-        });
-        return;
-    }
-    constexpr int K = piece_of(DT, V);
-    hipLaunchKernelGGL((k_gn_colparts_fwd<DT, V, K>), grid, block, cols_lds(p.cols, p.threads, 2, 1), st, xt, p.cols, n,
-                       parts);
-    if (!p.joined) combine_fwd(parts, int64_t(n) * p.cols.groups, p.cols.cg * p.pieces, eps, mean, rstd, st);
+    if (!p.held)
+        hipLaunchKernelGGL((k_gn_colparts_fwd<DT, V, piece_of(DT, V)>), grid, block, cols_lds(p.cols, p.threads, 2, 1), st, xt,
+                           p.cols, n, parts);
+    if (!p.held && !p.joined) combine_fwd(parts, int64_t(n) * p.cols.groups, p.cols.cg * p.pieces, eps, mean, rstd, st);
     with_act(q.act, [&](auto act) {
-        hipLaunchKernelGGL((k_gn_colwrite_fwd<DT, V, K, decltype(act)::value>), grid, block, joined_lds(p), st, xt, p.cols, n,
-                           q, mean, rstd, p.joined ? parts : nullptr, eps, yt);
+        with_past<DT, V, false>(p.cols, [&](auto past) {
+            constexpr int A = decltype(act)::value;
+            constexpr bool P = decltype(past)::value;
+            if (p.held)
+                with_count<DT, V, false>(p.k, [&](auto k) {
+                    hipLaunchKernelGGL((k_gn_cols_fwd<DT, V, decltype(k)::value, A, P>), grid, block,
+                                       cols_lds(p.cols, p.threads, 1, 2), st, xt, p.cols, n, q, eps, yt, mean, rstd);
+                });
+            else
+                hipLaunchKernelGGL((k_gn_colwrite_fwd<DT, V, piece_of(DT, V), A, P>), grid, block, joined_lds(p), st, xt,
+                                   p.cols, n, q, mean, rstd, p.joined ? parts : nullptr, eps, yt);
+        });
     });
 }
 
@@ -473,26 +483,28 @@ void bwd(const Plan& p, int n, const void* x, const void* dy, const Params& q, c
     const T *xt = static_cast<const T*>(x), *gt = static_cast<const T*>(dy);
     T* dt = static_cast<T*>(dx);
     const dim3 grid(static_cast<unsigned>(p.grid)), block(static_cast<unsigned>(p.threads));
-    if (p.held) {
-        with_act(q.act, [&](auto act) {
-            with_count<DT, V, true>(p.k, [&](auto k) {
-                hipLaunchKernelGGL((k_gn_cols_bwd<DT, V, decltype(k)::value, decltype(act)::value>), grid, block,
-                                   cols_lds(p.cols, p.threads, 2, 4), st, xt, gt, p.cols, n, q, mean, rstd, dt, sums);
-            });
-        });
-        return;
-    }
-    constexpr int K = piece_of(DT, V);
+    tail.first = grid.x;
     with_act(q.act, [&](auto act) {
-        hipLaunchKernelGGL((k_gn_colparts_bwd<DT, V, K, decltype(act)::value>), grid, block,
-                           cols_lds(p.cols, p.threads, 2, 0), st, xt, gt, p.cols, n, q, mean, rstd, sums.ab);
-        if (!p.joined)
+        constexpr int A = decltype(act)::value;
+        constexpr int K = piece_of(DT, V);
+        if (!p.held)
+            hipLaunchKernelGGL((k_gn_colparts_bwd<DT, V, K, A>), grid, block, cols_lds(p.cols, p.threads, 2, 0), st, xt, gt,
+                               p.cols, n, q, mean, rstd, sums.ab);
+        if (!p.held && !p.joined)
             combine_bwd(sums.ab, int64_t(n) * p.cols.groups, p.cols.cg * p.pieces, p.pieces, p.cols.groups, p.cols.cg,
                         float(p.cols.cg) * float(p.cols.hw), q.gamma, s12, st);
-        tail.first = grid.x;
-        hipLaunchKernelGGL((k_gn_colwrite_bwd<DT, V, K, decltype(act)::value>), dim3(grid.x + tail_blocks(tail)), block,
-                           joined_lds(p), st, xt, gt, p.cols, n, q, mean, rstd, s12, p.joined ? sums.ab : nullptr, tail,
-                           dt);
+        with_past<DT, V, true>(p.cols, [&](auto past) {
+            constexpr bool P = decltype(past)::value;
+            if (p.held)
+                with_count<DT, V, true>(p.k, [&](auto k) {
+                    hipLaunchKernelGGL((k_gn_cols_bwd<DT, V, decltype(k)::value, A, P>), grid, block,
+                                       cols_lds(p.cols, p.threads, 2, 4), st, xt, gt, p.cols, n, q, mean, rstd, dt, sums);
+                });
+            else
+                hipLaunchKernelGGL((k_gn_colwrite_bwd<DT, V, K, A, P>), dim3(grid.x + tail_blocks(tail)), block,
+                                   joined_lds(p), st, xt, gt, p.cols, n, q, mean, rstd, s12, p.joined ? sums.ab : nullptr,
+                                   tail, dt);
+        });
     });
 }
 

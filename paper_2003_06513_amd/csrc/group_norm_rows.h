@@ -46,7 +46,7 @@ __global__ __launch_bounds__(threads_of(DT, V, K)) void k_gn_rows_fwd(const type
     const Base<V, MASK> b(s, int64_t(blockIdx.x) * s.cg * s.hw);
     const int c0 = int(blockIdx.x % unsigned(s.groups)) * s.cg;
     typename P::R d[K];
-    each<V, MASK, K>(s, b, [&](int i, int, const Window& w, bool) { d[i] = load<DT, V, MASK>(x, b, w); }, Nothing());
+    each<V, MASK, K>(s, b, [&](int i, int, const Window& w, bool) { d[i] = load<DT, V, MASK, true>(x, b, w); }, Nothing());
     for (int row = threadIdx.x; row < s.cg; row += blockDim.x)
         row_params[row] = make_float2(or_one(q.gamma, c0 + row), or_zero(q.beta, c0 + row));
     float sum = 0.f;
@@ -105,8 +105,8 @@ __global__ __launch_bounds__(threads_of(DT, V, K)) void k_gn_rows_bwd(const type
     k.mu = mean[blockIdx.x], k.r = rstd[blockIdx.x];
     typename P::R d[K], e[K];
     each<V, MASK, K>(s, b, [&](int i, int, const Window& w, bool) {
-        d[i] = load<DT, V, MASK>(x, b, w);
-        e[i] = load<DT, V, MASK>(dy, b, w);
+        d[i] = load<DT, V, MASK, true>(x, b, w);
+        e[i] = load<DT, V, MASK, true>(dy, b, w);
     }, Nothing());
     for (int row = threadIdx.x; row < s.cg; row += blockDim.x)
         row_params[row] = make_float2(or_one(q.gamma, c0 + row), or_zero(q.beta, c0 + row));
@@ -218,7 +218,7 @@ __global__ __launch_bounds__(256, 4) void k_gn_rowparts_fwd(const typename Elt<D
     if (p.id >= count) return;
     const PieceBase<V, MASK> b(s, int64_t(p.row) * s.hw, p.piece * K * 64);
     typename P::R d[K];
-    each_of_piece<V, MASK, K>(b, [&](int i, const Window& w, bool) { d[i] = load<DT, V, MASK>(x, b, w); });
+    each_of_piece<V, MASK, K>(b, [&](int i, const Window& w, bool) { d[i] = load<DT, V, MASK, false>(x, b, w); });
     float sum = 0.f, num = 0.f;
     each_of_piece<V, MASK, K>(b, [&](int i, const Window& w, bool on) {
         float f[V], t = 0.f;
@@ -260,7 +260,7 @@ __global__ __launch_bounds__(256, 4) void k_gn_rowwrite_fwd(const typename Elt<D
     if (p.id >= count) return;
     const PieceBase<V, MASK> b(s, int64_t(p.row) * s.hw, p.piece * K * 64);
     typename P::R d[K];
-    each_of_piece<V, MASK, K>(b, [&](int i, const Window& w, bool) { d[i] = load<DT, V, MASK>(x, b, w); });
+    each_of_piece<V, MASK, K>(b, [&](int i, const Window& w, bool) { d[i] = load<DT, V, MASK, false>(x, b, w); });
     Coeff k{0.f, 0.f, or_one(q.gamma, p.c), or_zero(q.beta, p.c)};
     if (parts) {
         const int per = s.cg * pieces;
@@ -290,8 +290,8 @@ __global__ __launch_bounds__(256, MASK ? 3 : 4) void k_gn_rowparts_bwd(const typ
     const PieceBase<V, MASK> b(s, int64_t(p.row) * s.hw, p.piece * K * 64);
     typename P::R d[K], e[K];
     each_of_piece<V, MASK, K>(b, [&](int i, const Window& w, bool) {
-        d[i] = load<DT, V, MASK>(x, b, w);
-        e[i] = load<DT, V, MASK>(dy, b, w);
+        d[i] = load<DT, V, MASK, false>(x, b, w);
+        e[i] = load<DT, V, MASK, false>(dy, b, w);
     });
     const Coeff k = coeff_of(p, q, mean, rstd);
     float sa = 0.f, sb = 0.f;
@@ -328,8 +328,8 @@ __global__ __launch_bounds__(256, 4) void k_gn_rowwrite_bwd(const typename Elt<D
     const PieceBase<V, MASK> b(s, int64_t(p.row) * s.hw, p.piece * K * 64);
     typename P::R d[K], e[K];
     each_of_piece<V, MASK, K>(b, [&](int i, const Window& w, bool) {
-        d[i] = load<DT, V, MASK>(x, b, w);
-        e[i] = load<DT, V, MASK>(dy, b, w);
+        d[i] = load<DT, V, MASK, false>(x, b, w);
+        e[i] = load<DT, V, MASK, false>(dy, b, w);
     });
     const Coeff k = coeff_of(p, q, mean, rstd);
     const int per = s.cg * pieces;
