@@ -93,7 +93,7 @@ __device__ __forceinline__ void each_group(const Cols& q, int count, const float
     }
 }
 
-template <int DT, int V, int K, int ACT, bool PAST>
+template <int DT, int V, int K, int ACT, int PAST>
 __global__ __launch_bounds__(threads_of(DT, V, K)) void k_gn_cols_fwd(const typename Elt<DT>::T* __restrict__ x, Cols q,
                                                                   int images, Params w, float eps,
                                                                   typename Elt<DT>::T* __restrict__ y,
@@ -165,7 +165,7 @@ __global__ __launch_bounds__(threads_of(DT, V, K)) void k_gn_cols_fwd(const type
         P::open(d[i], f);
 #pragma unroll
         for (int j = 0; j < V; ++j) f[j] = forward<ACT>(Coeff{mu[j], r[j], ga[j], be[j]}, f[j]);
-        put<PAST>(y + at, byte, P::close(f));
+        put<PAST == 2>(y + at, byte, P::close(f));
     });
 }
 
@@ -207,7 +207,7 @@ __device__ __forceinline__ void sums_back(const typename Pack<DT, V>::R (&d)[K],
         }
     });
 }
-template <int DT, int V, int K, int ACT, bool PAST>
+template <int DT, int V, int K, int ACT, int PAST>
 __device__ __forceinline__ void write_back(const typename Pack<DT, V>::R (&d)[K], const typename Pack<DT, V>::R (&e)[K],
                                            const Cols& q, const Place& p, const Coeff (&k)[V], const Back (&s)[V],
                                            typename Elt<DT>::T* dxb) {
@@ -217,11 +217,11 @@ __device__ __forceinline__ void write_back(const typename Pack<DT, V>::R (&d)[K]
         Pack<DT, V>::open(e[i], g);
 #pragma unroll
         for (int j = 0; j < V; ++j) f[j] = backward<ACT>(k[j], s[j], f[j], g[j]);
-        put<PAST>(dxb, byte, Pack<DT, V>::close(f));
+        put<PAST == 2>(dxb, byte, Pack<DT, V>::close(f));
     });
 }
 
-template <int DT, int V, int K, int ACT, bool PAST>
+template <int DT, int V, int K, int ACT, int PAST>
 __global__ __launch_bounds__(threads_of(DT, V, K), 4) void k_gn_cols_bwd(const typename Elt<DT>::T* __restrict__ x,
                                                                      const typename Elt<DT>::T* __restrict__ dy, Cols q,
                                                                      int images, Params w,
@@ -240,8 +240,8 @@ __global__ __launch_bounds__(threads_of(DT, V, K), 4) void k_gn_cols_bwd(const t
     const typename Elt<DT>::T *xb = x + at, *gb = dy + at;
     typename P::R d[K], e[K];
     each<DT, K>(q, p, [&](int i, uint32_t byte) {
-        d[i] = get<typename P::R, PAST>(xb, byte);
-        e[i] = get<typename P::R, PAST>(gb, byte);
+        d[i] = get<typename P::R, (PAST > 0)>(xb, byte);
+        e[i] = get<typename P::R, (PAST > 0)>(gb, byte);
     });
     Coeff k[V];
     coefficients<V>(q, p, w, kept(q, p, mean, rstd), k);
@@ -327,7 +327,7 @@ template <class F> __device__ __forceinline__ void each_joined(const Cols& q, in
     for (int g = int(threadIdx.x) / q.join_lanes; g < count; g += int(blockDim.x) / q.join_lanes) f(g, lane);
 }
 
-template <int DT, int V, int K, int ACT, bool PAST>
+template <int DT, int V, int K, int ACT, int PAST>
 __global__ __launch_bounds__(256, 4) void k_gn_colwrite_fwd(const typename Elt<DT>::T* __restrict__ x, Cols q, int images,
                                                             Params w, float* __restrict__ mean,
                                                             float* __restrict__ rstd,
@@ -362,7 +362,7 @@ __global__ __launch_bounds__(256, 4) void k_gn_colwrite_fwd(const typename Elt<D
         P::open(d[i], f);
 #pragma unroll
         for (int j = 0; j < V; ++j) f[j] = forward<ACT>(k[j], f[j]);
-        put<PAST>(y + at, byte, P::close(f));
+        put<PAST == 2>(y + at, byte, P::close(f));
     });
 }
 
@@ -395,7 +395,7 @@ __global__ __launch_bounds__(256, 4) void k_gn_colparts_bwd(const typename Elt<D
             make_float2(sum_of_channel(lds, q, c), sum_of_channel(lds + all, q, c));
 }
 
-template <int DT, int V, int K, int ACT, bool PAST>
+template <int DT, int V, int K, int ACT, int PAST>
 __global__ __launch_bounds__(256, 4) void k_gn_colwrite_bwd(const typename Elt<DT>::T* __restrict__ x,
                                                          const typename Elt<DT>::T* __restrict__ dy, Cols q, int images,
                                                          Params w, const float* __restrict__ mean,
@@ -440,12 +440,17 @@ __global__ __launch_bounds__(256, 4) void k_gn_colwrite_bwd(const typename Elt<D
 // LDS of a block that joins its groups' pieces.
 unsigned joined_lds(const Plan& p) { return p.joined ? unsigned(sizeof(float2)) * unsigned(p.cols.tile / p.cols.cg) : 0u; }
 
-// Calls go with whether stores go past the caches: where they fill 64 bytes,
-// 128 in the backward, whose lanes write half as much (64 x 512 x 28 x 28 fp16
-// in tiles of 64 bytes 49 us, past the caches 52).
+// Calls go with what goes past the caches: 2, stores and what is read once,
+// where they fill 64 bytes; in the backward, whose lanes write half as much, the
+// stores where they fill 128 (64 x 512 x 28 x 28 fp16 in tiles of 64 bytes:
+// nothing 50 us, loads 46, both 49, stores 52).
 template <int DT, int V, bool BACK, class F> void with_past(const Cols& q, F go) {
-    if constexpr (V > 1)
-        if (q.tile * int(sizeof(typename Elt<DT>::T)) >= (BACK ? 128 : 64)) return go(IntC<1>{});
+    if constexpr (V > 1) {
+        const int bytes = q.tile * int(sizeof(typename Elt<DT>::T));
+        if (bytes >= (BACK ? 128 : 64)) return go(IntC<2>{});
+        if constexpr (BACK)
+            if (bytes >= 64) return go(IntC<1>{});
+    }
     go(IntC<0>{});
 }
 
@@ -463,7 +468,7 @@ void fwd(const Plan& p, int n, const void* x, const Params& q, float eps, void* 
     with_act(q.act, [&](auto act) {
         with_past<DT, V, false>(p.cols, [&](auto past) {
             constexpr int A = decltype(act)::value;
-            constexpr bool P = decltype(past)::value;
+            constexpr int P = decltype(past)::value;
             if (p.held)
                 with_count<DT, V, false>(p.k, [&](auto k) {
                     hipLaunchKernelGGL((k_gn_cols_fwd<DT, V, decltype(k)::value, A, P>), grid, block,
@@ -494,7 +499,7 @@ void bwd(const Plan& p, int n, const void* x, const void* dy, const Params& q, c
             combine_bwd(sums.ab, int64_t(n) * p.cols.groups, p.cols.cg * p.pieces, p.pieces, p.cols.groups, p.cols.cg,
                         float(p.cols.cg) * float(p.cols.hw), q.gamma, s12, st);
         with_past<DT, V, true>(p.cols, [&](auto past) {
-            constexpr bool P = decltype(past)::value;
+            constexpr int P = decltype(past)::value;
             if (p.held)
                 with_count<DT, V, true>(p.k, [&](auto k) {
                     hipLaunchKernelGGL((k_gn_cols_bwd<DT, V, decltype(k)::value, A, P>), grid, block,
