@@ -14,7 +14,9 @@
  *   psc_conv3x3_fwd     the pruned layer X_n = sigma(W_n X + b_n) Sec. 4.1, Eq. 1
  *
  * plus a dense comparator, a dense unpacker and the 2x2 max-pool of the
- * VGG-16 stack.
+ * VGG-16 stack; and of the training side the backward of the pruned layer,
+ * the data-free ADMM iteration, group normalisation, the gradients' norm and
+ * AdamW.
  *
  * Conventions for every entry point:
  *  - "d_" pointers are device memory, "h_" pointers host memory; all of it is
@@ -23,7 +25,8 @@
  *    `stream` (a hipStream_t, NULL = the null stream) and the caller keeps
  *    every buffer alive until that stream has drained it.
  *  - Weights are contiguous OIHW [cout][cin][3][3]; activations contiguous
- *    NCHW.  Masks are 9-bit codes, bit 3r+s for kernel row r, column s.
+ *    NCHW (group normalisation: or channels last).  Masks are 9-bit codes,
+ *    bit 3r+s for kernel row r, column s.
  *  - Arguments are validated synchronously, before any HIP call, so errors
  *    are reported the same way with or without a device.  A failed launch is
  *    returned as PSC_ERR_DEVICE.  No C++ exception crosses the ABI.
@@ -288,7 +291,8 @@ psc_status psc_conv3x3_bwd_weight(const psc_layer *layer, const psc_packed *pack
  * c / groups neighbouring channels, over its M = c / groups * h * w values:
  *   mean = sum x / M,  rstd = 1 / sqrt(sum (x - mean)^2 / M + eps),
  *   xhat = (x - mean) rstd,  u = gamma[c] xhat + beta[c],  y = act(u)
- * with act(u) = u, max(u, 0) or u / (1 + exp(-u)). */
+ * with act(u) = u, max(u, 0) or u / (1 + exp(-u)).  Nothing that a call writes
+ * (outputs, statistics, gradients, workspace) may overlap anything else of it. */
 typedef enum { PSC_NCHW = 0, PSC_NHWC = 1 } psc_layout;
 typedef enum { PSC_ACT_NONE = 0, PSC_ACT_RELU = 1, PSC_ACT_SILU = 2 } psc_act;
 
