@@ -63,10 +63,15 @@ struct Try {
 };
 constexpr Try kMany[] = {{64, 8}, {128, 8}, {256, 8}, {256, 16}, {512, 16}, {1024, 8}, {512, 32}};
 constexpr Try kFew[] = {{64, 4}, {128, 4}, {256, 4}, {512, 4}, {1024, 4}, {1024, 8}, {512, 16}, {512, 32}};
+// Columns that are more than the CUs but less than twice as many: of blocks of
+// 512 threads a CU runs two, of 1024 one, and then those that are left (9 x 512
+// x 28 x 28 fp32 backward, 288 blocks: 22.3 us, not 26.6; rows gain nothing).
+constexpr Try kSome[] = {{64, 4}, {128, 4}, {256, 4}, {512, 4}, {512, 8}, {512, 16}, {1024, 8}, {512, 32}};
 // The first of them that `count(threads)` vectors a thread fit, or none.
-template <class F> bool choose(int64_t units, int dtype, int v, bool backward, Plan& p, F count) {
-    const Try* list = units >= 512 ? kMany : kFew;
+template <class F> bool choose(int64_t units, bool cols, int dtype, int v, bool backward, Plan& p, F count) {
+    const Try* list = units >= 512 ? kMany : cols && units > 256 ? kSome : kFew;
     const int n = units >= 512 ? int(sizeof(kMany) / sizeof(Try)) : int(sizeof(kFew) / sizeof(Try));
+    static_assert(sizeof(kSome) == sizeof(kFew), "one count");
     for (int i = 0; i < n; ++i) {
         const int64_t k = count(list[i].threads);
         if (k < 1 || k > most_of(dtype, v, backward) || 16 * k > int64_t(list[i].part) * piece_of(dtype, v)) continue;
@@ -103,7 +108,7 @@ Plan plan_rows(const GroupNormArgs& a, bool backward, int vec) {
     p.vec = vec;
     p.grid = int64_t(a.n) * a.groups;
     if (vec && s.cg <= 2048 &&      // the rows' parameters and sums fit the LDS
-        choose(p.grid, a.dtype, v, backward, p, [&](int threads) {
+        choose(p.grid, false, a.dtype, v, backward, p, [&](int threads) {
             return rows_slots(s.cg, s.vpr, threads, &s.lanes_log2, &s.vi);
         })) {
         s.slots = p.k;
@@ -118,8 +123,25 @@ Plan plan_rows(const GroupNormArgs& a, bool backward, int vec) {
 int64_t cols_grid(Cols& s, int n, int elt) {
     s.near = 128 / (s.tile * elt);
     if (s.near < 1) s.near = 1;
-    if (s.near > s.tiles || int64_t(n) * s.chunks >= 64) s.near = s.tiles;
+    // whole images, where every die gets as many of them (48 x 512 x 28 x 28 fp32 backward 67 -> 56 us)
+    const int64_t images = int64_t(n) * s.chunks;
+    if (s.near > s.tiles || images >= 64 || (images >= 16 && images % 8 == 0)) s.near = s.tiles;
+    // slabs alike: of 12 tiles 6 and 6, not 8 and 4 (20 x 96 x 40 x 40 fp16 14.5 -> 12 us)
+    s.near = int(ceil_div(s.tiles, ceil_div(s.tiles, s.near)));
     return ceil_div(int64_t(n) * s.chunks * ceil_div(s.tiles, s.near), 8) * 8 * s.near;
+}
+
+// Whether tiles of less than half a line of memory lose.  Each of their lines
+// goes from the die's cache to several CUs, which long columns (k of `piece`
+// vectors a thread) pay for most: then wider tiles of fewer blocks, or pieces,
+// are faster once there are more blocks than CUs (forward, 20 x 256 x 56 x 56
+// fp32: 42 us in pieces, 57 held; 40 x 128 x 40 x 40 fp16: 14 in 160 blocks, 23
+// in 640), in the backward in tiles of 16 bytes also before (64 x 64 x 56 x
+// 56 fp16: 33 us in pieces, 41 held).
+bool narrow_loses(int64_t units, int threads, int64_t k, int bytes, bool wider, bool backward, int piece) {
+    const bool many = units > 256;
+    if (!backward) return many && (wider || 2 * k >= piece);
+    return (many && threads == 1024) || (bytes <= 16 && 4 * k > piece - (many ? 4 : 0));
 }
 
 Plan plan_cols(const GroupNormArgs& a, bool backward, int vec) {
@@ -140,11 +162,15 @@ Plan plan_cols(const GroupNormArgs& a, bool backward, int vec) {
         if (int64_t(s.hw) * a.c * elt >> 32) break;     // offsets of 32 bits
         const int64_t units = int64_t(a.n) * s.tiles;
         p.held = false;
-        if (choose(units, a.dtype, v, backward, p, [&](int threads) {
+        if (choose(units, true, a.dtype, v, backward, p, [&](int threads) {
                 if (threads < (1 << s.cols_log2) ||
                     cols_lds(s, threads, backward ? 2 : 1, backward ? 4 : 2) > 60 * 1024)
                     return int64_t(0);
-                return ceil_div(s.hw, threads >> s.cols_log2);
+                const int64_t k = ceil_div(s.hw, threads >> s.cols_log2);
+                if (vec && s.tile * elt < 64 && narrow_loses(units, threads, k, s.tile * elt, best.held, backward,
+                                                             piece_of(a.dtype, v)))
+                    return int64_t(0);
+                return k;
             })) {
             s.pixels = s.hw, s.chunks = 1;
             p.grid = cols_grid(s, a.n, elt);
