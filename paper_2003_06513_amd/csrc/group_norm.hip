@@ -6,20 +6,25 @@ namespace psc {
 namespace gn {
 namespace {
 
-// A block per group of many pieces.
-__global__ __launch_bounds__(256) void k_gn_combine_fwd(const float4* __restrict__ parts, int per, float eps,
+// A block per group of many pieces, of 1024 threads where they are more than
+// so many: 4 x 771 x 33 x 33 fp16, one group, channels last 40 -> 27 us.
+int combine_threads(int per) { return per > 1024 ? 1024 : 256; }
+
+__global__ __launch_bounds__(1024) void k_gn_combine_fwd(const float4* __restrict__ parts, int per, float eps,
                                                         float* __restrict__ mean, float* __restrict__ rstd) {
     __shared__ float part[32], again[16];
     const float4* p = parts + int64_t(blockIdx.x) * per;
     float sum = 0.f, num = 0.f;
-    for (int i = threadIdx.x; i < per; i += 256) {
+#pragma unroll 4
+    for (int i = threadIdx.x; i < per; i += blockDim.x) {
         sum = fmaf(p[i].z, p[i].x, sum);
         num += p[i].z;
     }
     const float2 both = block_sum2(num, sum, part);
     const float mu = both.y / both.x;
     float sq = 0.f;
-    for (int i = threadIdx.x; i < per; i += 256) {
+#pragma unroll 4
+    for (int i = threadIdx.x; i < per; i += blockDim.x) {
         const float d = p[i].x - mu;
         sq += fmaf(p[i].z * d, d, p[i].y);
     }
@@ -30,14 +35,15 @@ __global__ __launch_bounds__(256) void k_gn_combine_fwd(const float4* __restrict
     }
 }
 
-__global__ __launch_bounds__(256) void k_gn_combine_bwd(const float2* __restrict__ parts, int per, int pieces,
+__global__ __launch_bounds__(1024) void k_gn_combine_bwd(const float2* __restrict__ parts, int per, int pieces,
                                                         int groups, int cg, float m, const float* __restrict__ gamma,
                                                         float2* __restrict__ s12) {
     __shared__ float part[32];
     const float2* p = parts + int64_t(blockIdx.x) * per;
     const int c0 = int(blockIdx.x % unsigned(groups)) * cg;
     float s1 = 0.f, s2 = 0.f;
-    for (int i = threadIdx.x; i < per; i += 256) {
+#pragma unroll 4
+    for (int i = threadIdx.x; i < per; i += blockDim.x) {
         const float ga = or_one(gamma, c0 + i / pieces);
         s1 = fmaf(ga, p[i].x, s1);
         s2 = fmaf(ga, p[i].y, s2);
@@ -226,12 +232,13 @@ size_t bytes_of(const GroupNormArgs& a, bool backward, int vec) {
 }  // namespace
 
 void combine_fwd(const float4* parts, int64_t groups, int per_group, float eps, float* mean, float* rstd, hipStream_t st) {
-    hipLaunchKernelGGL(k_gn_combine_fwd, dim3(unsigned(groups)), dim3(256), 0, st, parts, per_group, eps, mean, rstd);
+    hipLaunchKernelGGL(k_gn_combine_fwd, dim3(unsigned(groups)), dim3(unsigned(combine_threads(per_group))), 0, st, parts,
+                       per_group, eps, mean, rstd);
 }
 void combine_bwd(const float2* parts, int64_t groups, int per_group, int pieces, int groups_per_image, int cg, float m,
                  const float* gamma, float2* s12, hipStream_t st) {
-    hipLaunchKernelGGL(k_gn_combine_bwd, dim3(unsigned(groups)), dim3(256), 0, st, parts, per_group, pieces,
-                       groups_per_image, cg, m, gamma, s12);
+    hipLaunchKernelGGL(k_gn_combine_bwd, dim3(unsigned(groups)), dim3(unsigned(combine_threads(per_group))), 0, st, parts,
+                       per_group, pieces, groups_per_image, cg, m, gamma, s12);
 }
 
 }  // namespace gn
