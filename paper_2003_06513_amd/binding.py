@@ -924,12 +924,20 @@ class AdamW:
         if self.scale is None:
             return self.m, self.v
         torch = _torch()
-        with torch.cuda.stream(_torch_stream(stream)):
-            m, v = (torch.empty(self.m.numel(), dtype=torch.float32, device=self.m.device) for _ in range(2))
+        total = self.m.numel()
+        both = lambda: [torch.empty(total, dtype=torch.float32, device=self.m.device) for _ in range(2)]    # noqa: E731
+        if stream is None:
+            m, v = both()
+        else:
+            with torch.cuda.stream(_torch_stream(stream)):
+                m, v = both()
         self._hold(stream)
         most = 1 << 30
-        for a in range(0, self.m.numel(), most):
-            b = min(a + most, self.m.numel())
+        if total <= most:
+            adamw_moments(self.m, self.v, self.scale, m, v, stream)
+            return m, v
+        for a in range(0, total, most):
+            b = min(a + most, total)
             adamw_moments(self.m[a:b], self.v[a:b], self.scale[a // ADAMW_GROUP:-(-b // ADAMW_GROUP)], m[a:b], v[a:b],
                           stream)
         return m, v

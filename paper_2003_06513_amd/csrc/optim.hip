@@ -19,6 +19,7 @@ namespace psc {
 namespace {
 
 typedef float f4 __attribute__((ext_vector_type(4)));
+typedef float f2 __attribute__((ext_vector_type(2)));
 typedef uint16_t h4 __attribute__((ext_vector_type(4)));
 typedef int8_t c4 __attribute__((ext_vector_type(4)));
 typedef uint8_t b4 __attribute__((ext_vector_type(4)));
@@ -27,26 +28,55 @@ typedef uint8_t b4 __attribute__((ext_vector_type(4)));
 // under 4 KiB).  Chunks of 1024 elements are numbered through the table, and a
 // block of a step takes one: blocks that go on to other chunks were slower (64
 // x 512 x 512 x 9 with 32 bits 869 us, not 783), as were chunks of 2048 (802).
-constexpr int kMaxEntries = 58;
+constexpr int kMaxEntries = 83;
 constexpr int kGroup = 256;       // elements that share the scales of 8-bit moments: 4 per lane of a wave
 constexpr int kNormBlocks = 1024; // partial sums of the norm (fixed: deterministic order)
+// Chunks that one block takes by itself, in one launch: 8.9 -> 5.9 us a call, in
+// a captured chain 4.2 -> 4.6; with 32 of them, of as many tensors, 4.2 -> 8.
+constexpr int kNormAlone = 16;
 
 enum : uint32_t { kWide = 1, kGradF16 = 2 };
 
+// A tensor in 44 bytes, so that many fit: the addresses' low and high halves
+// (they have 48 bits), the flags in bits that are free.  161 tensors, 10 M
+// elements with 8 bits: 42 us, with 58 entries of 64 bytes 45 (64 x 512 x 512 x
+// 9, where the bytes decide: 472 and 464).
+enum : int { kParam, kGrad, kCopy, kM, kV, kScale, kAddresses };
 struct Entry {
+    uint32_t lo[kAddresses], hi[kAddresses / 2];
+    uint32_t size;          // bit 31: kWide, every pointer is aligned for four elements
+    float wd;
+};
+// The same as the kernels use it.
+struct Tensor {
     float* p;
     const void* g;
     uint16_t* copy;
-    void* m;
-    void* v;
+    void *m, *v;
     float2* scale;
-    uint32_t numel;
+    uint32_t numel, flags;
     float wd;
-    uint32_t flags;      // kWide: every pointer is aligned for four elements
 };
+template <class T> __device__ __forceinline__ T* address(const Entry& e, int k, uint32_t clear = 0u) {
+    const uint32_t high = e.hi[k / 2] >> (16 * (k & 1)) & 0xffffu;
+    // as an address of global memory: loads and stores of any would go by the LDS too
+    return (T*)(__attribute__((address_space(1))) T*)(uint64_t(high) << 32 | (e.lo[k] & ~clear));
+}
+__device__ __forceinline__ Tensor tensor(const Entry& e) {
+    Tensor t;
+    t.p = address<float>(e, kParam);
+    t.g = address<const void>(e, kGrad, 1u);
+    t.copy = address<uint16_t>(e, kCopy);
+    t.m = address<void>(e, kM), t.v = address<void>(e, kV);
+    t.scale = address<float2>(e, kScale);
+    t.numel = e.size & 0x7fffffffu;
+    t.flags = (e.size >> 31 ? kWide : 0u) | (e.lo[kGrad] & 1u ? kGradF16 : 0u);
+    t.wd = e.wd;
+    return t;
+}
 // first[i]: the first chunk of tensor i; where there is none, past all chunks.
 struct Table {
-    uint32_t first[64];
+    uint32_t first[kMaxEntries + 1];
     Entry e[kMaxEntries];
     int32_t n;
     uint32_t chunks;
@@ -64,7 +94,7 @@ struct GradTable {
     int32_t n;
     uint32_t chunks;
 };
-static_assert(kMaxEntries <= 64 && sizeof(Table) <= 4000 && sizeof(GradTable) <= 4000, "kernel arguments");
+static_assert(sizeof(Entry) == 44 && sizeof(Table) <= 4000 && sizeof(GradTable) <= 4000, "kernel arguments");
 
 // The caller's state.  The last block of a step's last launch to read the
 // count raises it.  The blocks are counted at kEnds words, each in a line of
@@ -126,11 +156,24 @@ __device__ __forceinline__ Now now(const Hyper& hp, State* st, bool last) {
 // The tensor that chunk c belongs to: every lane looks at one tensor's first
 // chunk (or a few), so that one load is waited for; a binary search waits for
 // one after the other (161 tensors, 10 M elements with 8 bits: 57 us, not 53).
-template <int N> __device__ __forceinline__ int find_entry(const uint32_t (&first)[N], uint32_t c) {
+struct Found {
+    int at;
+    uint32_t first;
+};
+template <int N> __device__ __forceinline__ Found find_entry(const uint32_t (&first)[N], uint32_t c) {
+    constexpr int R = (N + 63) / 64;
+    const int lane = int(threadIdx.x & 63);
+    uint32_t f[R];
+#pragma unroll
+    for (int i = 0; i < R; ++i) f[i] = first[i * 64 + lane < N ? i * 64 + lane : N - 1];
     int at = -1;
 #pragma unroll
-    for (int i = 0; i < N; i += 64) at += __popcll(__ballot(first[i + (threadIdx.x & 63)] <= c));
-    return __builtin_amdgcn_readfirstlane(at);
+    for (int i = 0; i < R; ++i) at += __popcll(__ballot((i * 64 + lane < N) & (f[i] <= c)));
+    at = __builtin_amdgcn_readfirstlane(at);
+    uint32_t v = f[0];
+#pragma unroll
+    for (int i = 1; i < R; ++i) v = at >= i * 64 ? f[i] : v;
+    return Found{at, uint32_t(__builtin_amdgcn_readlane(int(v), at & 63))};
 }
 
 // Four elements, as far as there are any.  What a step reads and writes goes
@@ -168,11 +211,19 @@ __device__ __forceinline__ f4 widened(const h4& h) {
     }
     return r;
 }
+// Four gradients as they lie in memory; opened where they are needed, so that
+// nothing is waited for between the loads of a block.
 template <bool PAST>
 __device__ __forceinline__ f4 load_grad(const void* g, int64_t i, int left, uint32_t flags) {
     const bool wide = flags & kWide;
     if (!(flags & kGradF16)) return load4<f4, PAST>(static_cast<const float*>(g) + i, left, wide);
-    return widened(load4<h4, PAST>(static_cast<const uint16_t*>(g) + i, left, wide));
+    const f2 raw = __builtin_bit_cast(f2, load4<h4, PAST>(static_cast<const uint16_t*>(g) + i, left, wide));
+    return f4{raw.x, raw.y, 0.f, 0.f};
+}
+__device__ __forceinline__ f4 opened(const f4& raw, uint32_t flags) {
+    if (!(flags & kGradF16)) return raw;
+    const f2 half = {raw.x, raw.y};
+    return widened(__builtin_bit_cast(h4, half));
 }
 
 // p from the new moments.  The quotient by v_rcp_f32 and v_sqrt_f32, each
@@ -191,17 +242,18 @@ __global__ void k_adamw_none(const float* __restrict__ factor, State* __restrict
 
 // Four elements in a row per lane.
 __global__ __launch_bounds__(256) void k_adamw32(Table tab, Hyper hp, State* __restrict__ st, bool last) {
-    const int at = find_entry(tab.first, blockIdx.x);
-    const Entry& e = tab.e[at];
-    const uint32_t i = (blockIdx.x - tab.first[at]) * 1024 + threadIdx.x * 4;
+    const Found found = find_entry(tab.first, blockIdx.x);
+    const Tensor e = tensor(tab.e[found.at]);
+    const uint32_t i = (blockIdx.x - found.first) * 1024 + threadIdx.x * 4;
     const int left = i >= e.numel ? 0 : e.numel - i < 4 ? int(e.numel - i) : 4;
     const bool wide = e.flags & kWide;
     float* mp = static_cast<float*>(e.m) + i;
     float* vp = static_cast<float*>(e.v) + i;
-    const f4 g = load_grad<true>(e.g, i, left, e.flags);
+    const f4 raw = load_grad<true>(e.g, i, left, e.flags);
     f4 p = load4<f4, true>(e.p + i, left, wide), m = load4<f4, true>(mp, left, wide), v = load4<f4, true>(vp, left, wide);
     const Now n = now(hp, st, last);        // while those are on their way
     if (!n.go) return;
+    const f4 g = opened(raw, e.flags);
     const float decay = n.lr * e.wd;
     h4 h;
 #pragma unroll
@@ -266,21 +318,22 @@ __device__ __forceinline__ uint32_t magnitude_bits(float x) { return __builtin_b
 
 // One group per wave: lane l has the elements 4 l .. 4 l + 3 of it.
 __global__ __launch_bounds__(256) void k_adamw8(Table tab, Hyper hp, State* __restrict__ st, bool last) {
-    const int at = find_entry(tab.first, blockIdx.x);
-    const Entry& e = tab.e[at];
-    const uint32_t group = (blockIdx.x - tab.first[at]) * 4 + (threadIdx.x >> 6), lane4 = (threadIdx.x & 63) * 4;
+    const Found found = find_entry(tab.first, blockIdx.x);
+    const Tensor e = tensor(tab.e[found.at]);
+    const uint32_t group = (blockIdx.x - found.first) * 4 + (threadIdx.x >> 6), lane4 = (threadIdx.x & 63) * 4;
     const uint32_t i = group * kGroup + lane4;
     const int left = i >= e.numel ? 0 : e.numel - i < 4 ? int(e.numel - i) : 4;
     const bool wide = e.flags & kWide;
     int8_t* mp = static_cast<int8_t*>(e.m) + i;
     uint8_t* vp = static_cast<uint8_t*>(e.v) + i;
-    const float2 peak = group * kGroup < e.numel ? e.scale[group] : make_float2(0.f, 0.f);
-    const f4 g = load_grad<true>(e.g, i, left, e.flags);
+    const float2 peak = e.scale[group * kGroup < e.numel ? group : 0];
+    const f4 raw = load_grad<true>(e.g, i, left, e.flags);
     f4 p = load4<f4, true>(e.p + i, left, wide);
     c4 qm = load4<c4, true>(mp, left, wide);
     b4 qv = load4<b4, true>(vp, left, wide);
     const Now n = now(hp, st, last);        // while those are on their way
     if (!n.go || group * kGroup >= e.numel) return;     // the whole wave
+    const f4 g = opened(raw, e.flags);
     const float decay = n.lr * e.wd;
     const double factor = n.factor;
     const double km = hp.b1 * (1.0 / kTopM) * peak.x, kv = hp.b2 * (1.0 / kTopV) * peak.y,
@@ -344,12 +397,14 @@ __global__ __launch_bounds__(256) void k_moments(const int8_t* __restrict__ qm, 
 // with one for every element 64 x 512 x 512 x 9 took 164 us).  Sums in 64
 // bits; one partial sum per block, added in a fixed order.
 __device__ __forceinline__ double block_sum(double x) {
-    __shared__ double part[4];
+    __shared__ double part[16];
 #pragma unroll
     for (int off = 32; off > 0; off >>= 1) x += __shfl_xor(x, off);
     if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = x;
     __syncthreads();
-    return (part[0] + part[1]) + (part[2] + part[3]);
+    x = 0.0;
+    for (unsigned i = 0; i < blockDim.x >> 6; i += 4) x += (part[i] + part[i + 1]) + (part[i + 2] + part[i + 3]);
+    return x;
 }
 
 __device__ __forceinline__ double squares(const f4& g, bool half, double acc) {
@@ -359,20 +414,35 @@ __device__ __forceinline__ double squares(const f4& g, bool half, double acc) {
     return acc;
 }
 
-// The block's chunks lie side by side, so that it goes through the table once;
-// inside a tensor it loads kAhead of them before it adds the first (one by one
+struct Clip {
+    float scale, max_norm;
+    float* out;
+};
+__device__ __forceinline__ void clip(const Clip& k, double squares) {
+    const double norm = double(k.scale) * sqrt(squares);
+    k.out[0] = float(norm);
+    // a norm that is not finite has no factor: the step that reads it leaves everything as it was
+    k.out[1] = !__builtin_isfinite(float(norm))
+                   ? __builtin_nanf("")
+                   : float(double(k.scale) * (norm > double(k.max_norm) ? double(k.max_norm) / norm : 1.0));
+}
+
+// 256 threads' chunks lie side by side, so that they go through the table once;
+// inside a tensor they load kAhead of them before it adds the first (one by one
 // too little is on its way: 64 x 512 x 512 x 9 fp16 115 us, not 51).
 constexpr int kAhead = 8;
-__global__ __launch_bounds__(256) void k_norm_parts(GradTable tab, bool add, double* __restrict__ part) {
+template <int THREADS>
+__global__ __launch_bounds__(THREADS) void k_norm_parts(GradTable tab, bool add, double* __restrict__ part, Clip alone) {
     double acc = 0.0;
-    const uint32_t per = (tab.chunks + gridDim.x - 1) / gridDim.x;
-    uint32_t c = blockIdx.x * per;
+    const uint32_t all = gridDim.x * (THREADS / 256), per = (tab.chunks + all - 1) / all;
+    // the same for a whole wave, which the compiler has to know: 51 us, not 76, on 64 x 512 x 512 x 9 fp16
+    uint32_t c = (blockIdx.x * (THREADS / 256) + uint32_t(__builtin_amdgcn_readfirstlane(int(threadIdx.x >> 8)))) * per;
     const uint32_t c1 = c + per < tab.chunks ? c + per : tab.chunks;
-    int at = find_entry(tab.first, c);
+    Found found = find_entry(tab.first, c);
     while (c < c1) {
-        if (at + 1 < tab.n && tab.first[at + 1] == c) ++at;      // every tensor of the table has a chunk
-        const GradEntry& e = tab.e[at];
-        const uint32_t chunk = c - tab.first[at], i = chunk * 1024 + threadIdx.x * 4;
+        if (found.at + 1 < tab.n && tab.first[found.at + 1] == c) ++found.at, found.first = c;      // every tensor of the table has a chunk
+        const GradEntry& e = tab.e[found.at];
+        const uint32_t chunk = c - found.first, i = chunk * 1024 + (threadIdx.x & 255) * 4;
         const bool half = e.flags & kGradF16;
         if ((e.flags & kWide) && c + kAhead <= c1 && (chunk + kAhead) * 1024 <= e.numel) {
             if (half) {
@@ -390,26 +460,21 @@ __global__ __launch_bounds__(256) void k_norm_parts(GradTable tab, bool add, dou
             }
             c += kAhead;
         } else {
-            if (i < e.numel) acc = squares(load_grad<false>(e.g, i, e.numel - i < 4 ? int(e.numel - i) : 4, e.flags), half, acc);
+            if (i < e.numel) acc = squares(opened(load_grad<false>(e.g, i, e.numel - i < 4 ? int(e.numel - i) : 4, e.flags), e.flags), half, acc);
             ++c;
         }
     }
     acc = block_sum(acc);
-    if (threadIdx.x == 0) part[blockIdx.x] = add ? part[blockIdx.x] + acc : acc;
+    if (threadIdx.x != 0) return;
+    if (alone.out) clip(alone, acc);
+    else part[blockIdx.x] = add ? part[blockIdx.x] + acc : acc;
 }
 
-__global__ __launch_bounds__(256) void k_norm_end(const double* __restrict__ part, int n, float scale, float max_norm,
-                                                  float* __restrict__ out) {
+__global__ __launch_bounds__(256) void k_norm_end(const double* __restrict__ part, int n, Clip k) {
     double acc = 0.0;
     for (int i = threadIdx.x; i < n; i += 256) acc += part[i];
     acc = block_sum(acc);
-    if (threadIdx.x == 0) {
-        const double norm = double(scale) * sqrt(acc);
-        out[0] = float(norm);
-        // a norm that is not finite has no factor: the step that reads it leaves everything as it was
-        out[1] = !__builtin_isfinite(float(norm)) ? __builtin_nanf("")
-                                                  : float(double(scale) * (norm > double(max_norm) ? double(max_norm) / norm : 1.0));
-    }
+    if (threadIdx.x == 0) clip(k, acc);
 }
 
 bool aligned(const void* p, size_t a) { return reinterpret_cast<uintptr_t>(p) % a == 0; }
@@ -448,9 +513,13 @@ hipError_t launch_grad_norm(const ParamView* q, int count, float scale, float ma
     int64_t all = 0;
     for (int i = 0; i < count; ++i) all += chunks_of(q[i]);
     const int grid = int(all < 1 ? 1 : all < kNormBlocks ? all : kNormBlocks);
+    const Clip whole{scale, max_norm, out}, none{scale, max_norm, nullptr};
     bool add = false;
     const auto flush = [&] {
-        hipLaunchKernelGGL(k_norm_parts, dim3(unsigned(grid)), dim3(256), 0, stream, tab, add, part);
+        if (all <= kNormAlone)
+            hipLaunchKernelGGL(k_norm_parts<1024>, dim3(1), dim3(1024), 0, stream, tab, add, part, whole);
+        else
+            hipLaunchKernelGGL(k_norm_parts<256>, dim3(unsigned(grid)), dim3(256), 0, stream, tab, add, part, none);
         add = true;
         clear(tab);
     };
@@ -461,7 +530,7 @@ hipError_t launch_grad_norm(const ParamView* q, int count, float scale, float ma
         add_entry(tab, GradEntry{q[i].grad, uint32_t(q[i].numel), grad_flags(q[i])}, ch);
     }
     if (tab.n || !add) flush();
-    hipLaunchKernelGGL(k_norm_end, dim3(1), dim3(256), 0, stream, part, grid, scale, max_norm, out);
+    if (all > kNormAlone) hipLaunchKernelGGL(k_norm_end, dim3(1), dim3(256), 0, stream, part, grid, whole);
     return hipGetLastError();
 }
 
@@ -492,9 +561,18 @@ hipError_t launch_adamw(const ParamView* q, int count, const AdamwArgs& a, const
             const size_t am = bits == 32 ? 16 : 4;
             if (!aligned(q[i].param, 16) || !aligned(q[i].m, am) || !aligned(q[i].v, am) || !aligned(q[i].copy, 8))
                 flags &= ~uint32_t(kWide);
-            add_entry(tab, Entry{q[i].param, q[i].grad, static_cast<uint16_t*>(q[i].copy), q[i].m, q[i].v,
-                                 static_cast<float2*>(static_cast<void*>(q[i].scale)), uint32_t(q[i].numel),
-                                 q[i].weight_decay, flags}, ch);
+            const void* at[kAddresses] = {q[i].param, q[i].grad, q[i].copy, q[i].m, q[i].v, bits == 8 ? q[i].scale : nullptr};
+            Entry e{};
+            for (int k = 0; k < kAddresses; ++k) {
+                const uint64_t a = reinterpret_cast<uintptr_t>(at[k]);
+                if (a >> 48) return hipErrorInvalidDevicePointer;
+                e.lo[k] = uint32_t(a);
+                e.hi[k / 2] |= uint32_t(a >> 32) << (16 * (k & 1));
+            }
+            if (flags & kGradF16) e.lo[kGrad] |= 1u;
+            e.size = uint32_t(q[i].numel) | (flags & kWide ? 1u << 31 : 0u);
+            e.wd = q[i].weight_decay;
+            add_entry(tab, e, ch);
             --left[bits == 8];
         }
         if (tab.n) flush(bits);

@@ -53,7 +53,7 @@ def _flat(arrays, shift, guard, dtype=None):
 
 
 LISTS = [[1], [5, 0, 256, 257, 3], [1024, 1023, 4097, 64], [70001, 12], list(range(1, 120)), [300_000, 5, 262_144],
-         [7] * 400]
+         [7] * 400, [1024] * 16, [1000] * 17, [16384], [300] * 83, [300] * 84]
 
 
 @pytest.mark.parametrize("half", [False, True])
