@@ -154,9 +154,15 @@ def _check(rc: int, where: str):
 
 
 # ------------------------------------------------------------------ helpers
+_TORCH = None
+
+
 def _torch():
-    import torch
-    return torch
+    global _TORCH
+    if _TORCH is None:
+        import torch
+        _TORCH = torch
+    return _TORCH
 
 
 def dtype_code(t) -> int:
@@ -178,12 +184,13 @@ def _dev(t, name):
     return t.data_ptr() if t.numel() else None
 
 
-def _stream(stream):
-    """The handle of ``stream`` (None: the current one of the current device)."""
+def _stream(stream, device=None):
+    """The handle of ``stream`` (None: the current one of the current device,
+    whose index is ``device`` where the caller knows it)."""
     if stream is not None:
         return stream.cuda_stream
     torch = _torch()
-    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device() if device is None else device)
 
 
 def _torch_stream(stream):
@@ -623,16 +630,14 @@ class AdmmLayer:
 
 
 # ------------------------------------------------------------------ group normalisation
-def _current_device() -> int:
-    return _torch().cuda.current_device()
-
-
-def _same_device(*tensors):
-    """The tensors of a call lie on the current device, whose streams it runs on."""
-    at = _current_device()
+def _same_device(*tensors) -> int:
+    """The tensors of a call lie on the current device, whose streams it runs
+    on: its index."""
+    at = _torch()._C._cuda_getDevice()
     for t in tensors:
         if t is not None and t.get_device() != at:
             raise ValueError("a tensor lies on %s, and the current device is cuda:%d" % (t.device, at))
+    return at
 
 
 def _layout(x) -> int:
@@ -646,20 +651,22 @@ def _layout(x) -> int:
     raise ValueError("x must be contiguous, in NCHW or with the channels last")
 
 
-def _like(t, x, layout, name):
-    """The address of ``t``, which has the shape, type, layout and device of ``x``."""
+def _like(t, x, layout, name, device=None):
+    """The address of ``t``, which has the shape, type, layout and device (its index: ``device``) of ``x``."""
     torch = _torch()
-    if t.dtype != x.dtype or t.shape != x.shape or t.get_device() != x.get_device() or not t.is_contiguous(
-            memory_format=torch.channels_last if layout == PSC_NHWC else torch.contiguous_format):
+    if device is None:
+        device = x.get_device()
+    if t.dtype is not x.dtype or t.get_device() != device or t.shape != x.shape or not (t.is_contiguous(
+            memory_format=torch.channels_last) if layout else t.is_contiguous()):
         raise ValueError("%s must have the shape, type, layout and device of x" % name)
-    return t.data_ptr() or None
+    return t.data_ptr()
 
 
-def _vector(t, numel, x, name):
-    """The address of the fp32 values ``t`` (may be None) on the device of ``x``."""
+def _vector(t, numel, device, name):
+    """The address of the fp32 values ``t`` (may be None) on ``device`` (its index)."""
     if t is None:
         return None
-    if t.dtype != _torch().float32 or t.numel() != numel or t.get_device() != x.get_device() or not t.is_contiguous():
+    if t.dtype is not _torch().float32 or t.numel() != numel or t.get_device() != device or not t.is_contiguous():
         raise ValueError("%s must have %d contiguous float32 elements on the device of x" % (name, numel))
     return t.data_ptr() or None
 
@@ -709,16 +716,15 @@ def group_norm_fwd(x, groups: int, gamma, beta, y, eps: float = 1e-5, act: str =
     of channels of x [n, c, h, w], contiguous or channels_last (y the same);
     gamma and beta (fp32, or None), and mean and rstd (fp32 [n, groups], or
     None), which group_norm_bwd reads.  act: "none", "relu" or "silu"."""
-    layout, dt = _layout(x), dtype_code(x)
+    layout, dt, at = _layout(x), dtype_code(x), _same_device(x)
     n, c, h, w = x.shape
     groups = int(groups)
-    _same_device(x)
-    xp, yp = x.data_ptr(), _like(y, x, layout, "y") or 0
+    xp, yp = x.data_ptr(), _like(y, x, layout, "y", at)
     wp, wb, ws = _norm_scratch(ws, stream, dt, layout, n, c, h, w, groups, False, not (xp | yp) & 15)
-    _check(lib().psc_group_norm_fwd(dt, layout, xp, n, c, h, w, groups, _vector(gamma, c, x, "gamma"),
-                                    _vector(beta, c, x, "beta"), eps, _act_code(act), yp,
-                                    _vector(mean, n * groups, x, "mean"), _vector(rstd, n * groups, x, "rstd"), wp, wb,
-                                    _stream(stream)), "psc_group_norm_fwd")
+    _check(lib().psc_group_norm_fwd(dt, layout, xp, n, c, h, w, groups, _vector(gamma, c, at, "gamma"),
+                                    _vector(beta, c, at, "beta"), eps, _act_code(act), yp,
+                                    _vector(mean, n * groups, at, "mean"), _vector(rstd, n * groups, at, "rstd"), wp, wb,
+                                    _stream(stream, at)), "psc_group_norm_fwd")
 
 
 def group_norm_bwd(x, dy, groups: int, gamma, beta, mean, rstd, dx, dgamma=None, dbeta=None, act: str = "none",
@@ -726,17 +732,16 @@ def group_norm_bwd(x, dy, groups: int, gamma, beta, mean, rstd, dx, dgamma=None,
     """psc_group_norm_bwd: dx, and dgamma and dbeta (fp32 [c], or None), from
     the gradient dy of group_norm_fwd's output and the statistics that it
     wrote; dy and dx have the type and layout of x."""
-    layout, dt = _layout(x), dtype_code(x)
+    layout, dt, at = _layout(x), dtype_code(x), _same_device(x)
     n, c, h, w = x.shape
     groups = int(groups)
-    _same_device(x)
-    xp, gp, dp = x.data_ptr(), _like(dy, x, layout, "dy") or 0, _like(dx, x, layout, "dx") or 0
+    xp, gp, dp = x.data_ptr(), _like(dy, x, layout, "dy", at), _like(dx, x, layout, "dx", at)
     wp, wb, ws = _norm_scratch(ws, stream, dt, layout, n, c, h, w, groups, True, not (xp | gp | dp) & 15)
-    _check(lib().psc_group_norm_bwd(dt, layout, xp, gp, n, c, h, w, groups, _vector(gamma, c, x, "gamma"),
-                                    _vector(beta, c, x, "beta"), _vector(mean, n * groups, x, "mean"),
-                                    _vector(rstd, n * groups, x, "rstd"), _act_code(act), dp,
-                                    _vector(dgamma, c, x, "dgamma"), _vector(dbeta, c, x, "dbeta"), wp, wb,
-                                    _stream(stream)), "psc_group_norm_bwd")
+    _check(lib().psc_group_norm_bwd(dt, layout, xp, gp, n, c, h, w, groups, _vector(gamma, c, at, "gamma"),
+                                    _vector(beta, c, at, "beta"), _vector(mean, n * groups, at, "mean"),
+                                    _vector(rstd, n * groups, at, "rstd"), _act_code(act), dp,
+                                    _vector(dgamma, c, at, "dgamma"), _vector(dbeta, c, at, "dbeta"), wp, wb,
+                                    _stream(stream, at)), "psc_group_norm_bwd")
 
 
 # ------------------------------------------------------------------ the optimiser
@@ -811,23 +816,22 @@ class ParamList:
             self.c[i].grad, self.c[i].grad_dtype = addresses[i], codes[i]
         self.grads = grads
 
-    def check_device(self):
-        if self.count:
-            _same_device(self.grads[0])
+    def one(self):
+        """A tensor of the list (they all lie on one device), or None."""
+        return self.grads[0] if self.count else None
 
 
 def grad_norm(params: ParamList, out, max_norm: float = float("inf"), scale: float = 1.0, ws=None, stream=None):
     """psc_grad_norm: out (fp32 [2], device) = the norm of all gradients times
     ``scale``, and the factor that unscales and clips them to ``max_norm``
     (NaN if the norm is not finite)."""
-    params.check_device()
-    _same_device(out, ws)
+    at = _same_device(params.one(), out, ws)
     if out.numel() != 2:
         raise ValueError("out must have 2 elements")
     if ws is None:
         ws = _scratch(GRAD_NORM_WS_BYTES, stream)
     _check(lib().psc_grad_norm(params.c, params.count, float(scale), float(max_norm), _f32(out, "out"), _dev(ws, "ws"),
-                               _ws_bytes(ws), _stream(stream)), "psc_grad_norm")
+                               _ws_bytes(ws), _stream(stream, at)), "psc_grad_norm")
 
 
 def adamw_step(params: ParamList, state, lr, betas=(0.9, 0.999), eps: float = 1e-8, factor=None, stream=None):
@@ -835,9 +839,8 @@ def adamw_step(params: ParamList, state, lr, betas=(0.9, 0.999), eps: float = 1e
     device tensor of ADAMW_STATE_BYTES bytes, zeros before the first step; ``lr``: a number,
     or an fp32 device tensor that the step reads; ``factor``: None, or an fp32
     device tensor whose first element the gradients are multiplied by."""
-    params.check_device()
     on_device = hasattr(lr, "data_ptr")
-    _same_device(state, factor, lr if on_device else None)
+    at = _same_device(params.one(), state, factor, lr if on_device else None)
     for t, name in ((factor, "factor"), (lr if on_device else None, "lr")):
         if t is not None and t.numel() < 1:
             raise ValueError("%s must have an element" % name)
@@ -846,7 +849,7 @@ def adamw_step(params: ParamList, state, lr, betas=(0.9, 0.999), eps: float = 1e
     opt = CAdamW(0.0 if on_device else float(lr), float(betas[0]), float(betas[1]), float(eps),
                  _f32(lr, "lr") if on_device else None)
     _check(lib().psc_adamw_step(params.c, params.count, ctypes.byref(opt), _f32(factor, "factor"), _dev(state, "state"),
-                                _stream(stream)), "psc_adamw_step")
+                                _stream(stream, at)), "psc_adamw_step")
 
 
 def adamw_moments(m, v, scale, m_out, v_out, stream=None):
