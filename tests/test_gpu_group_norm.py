@@ -139,6 +139,9 @@ SHAPES = [
     ((2, 32, 64, 64), 1),               # one large group an image
     ((1, 16, 112, 112), 4), ((1, 8, 224, 224), 4), ((2, 6, 181, 193), 2),   # large planes
     ((3, 128, 28, 28), 32), ((40, 64, 16, 16), 32), ((2, 256, 56, 56), 32),
+    ((9, 512, 14, 14), 32), ((20, 96, 40, 40), 24), ((40, 64, 40, 40), 32),     # between one and a few blocks a CU
+    ((16, 32, 20, 20), 8), ((24, 48, 9, 10), 4),                                # whole images on a die
+    ((4, 771, 12, 12), 1), ((3, 778, 11, 11), 2), ((2, 512, 14, 14), 1),        # many short rows of a group
 ]
 
 
