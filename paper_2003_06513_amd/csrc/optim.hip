@@ -283,36 +283,63 @@ __global__ __launch_bounds__(256) void k_adamw32(Table tab, Hyper hp, State* __r
 // with code 0 the next step would divide by eps alone.
 constexpr double kTopM = 127.0 * 127.0, kTopV = 255.0 * 255.0 * 255.0 * 255.0;
 
+// Whole numbers in 64 bits: laid behind the exponent of 2^52 and that taken
+// away.  A conversion takes as long as four such operations; with them, the
+// peaks by the LDS and a division each 64 x 512 x 512 x 9 took 456 us, not 443.
+__device__ __forceinline__ double whole(uint32_t n) {
+    return __builtin_bit_cast(double, uint64_t(0x43300000u) << 32 | n) - 0x1p52;
+}
+__device__ __forceinline__ double whole_signed(int n) {
+    return __builtin_bit_cast(double, uint64_t(0x43300000u) << 32 | (uint32_t(n) ^ 0x80000000u)) - (0x1p52 + 0x1p31);
+}
 // q |q| and c^4, which times the scale and 1 / kTop are the values.
-__device__ __forceinline__ double power_m(int q) { return double(q * (q < 0 ? -q : q)); }
+__device__ __forceinline__ double power_m(int q) { return whole_signed(q * (q < 0 ? -q : q)); }
 __device__ __forceinline__ double power_v(uint32_t c) {
     const uint32_t s = c * c;
-    return double(s * s);
+    return whole(s * s);
 }
-// The root is raised by more than its error, so that the code is right or one
-// too high; one look at the border below (its square is exact in fp32) tells which.
-__device__ __forceinline__ int encode_m(double t) {
-    int c = int(fmaf(__builtin_amdgcn_sqrtf(float(t)), 1.f + 0x1p-20f, 0.5f));
-    const float b = float(c) - 0.5f;
-    c -= c > 0 && double(b * b) > t;
+// Codes from 4 |m| 127^2 / a and 16 v 255^4 / a, and these in 32 bits.  The
+// root is raised by more than its error, so that the code is right or one too
+// high; one look at the border below, (2 c - 1)^2 or ^4, tells which.
+__device__ __forceinline__ int encode_m(double t4, float near) {
+    int c = int(fmaf(__builtin_amdgcn_sqrtf(near), 0.5f + 0x1p-21f, 0.5f));
+    const uint32_t b = uint32_t(2 * c - 1) & 0x3ffu;
+    c -= c > 0 && whole(b * b) > t4;
     return c > 127 ? 127 : c;
 }
-__device__ __forceinline__ int encode_v(double t) {
-    int c = int(fmaf(__builtin_amdgcn_sqrtf(__builtin_amdgcn_sqrtf(float(t))), 1.f + 0x1p-20f, 0.5f));
-    const float b = float(c) - 0.5f;
-    const double bb = double(b * b);
-    c -= c > 0 && bb * bb > t;
+__device__ __forceinline__ int encode_v(double t16, float near) {
+    int c = int(fmaf(__builtin_amdgcn_sqrtf(__builtin_amdgcn_sqrtf(near)), 0.5f + 0x1p-21f, 0.5f));
+    const uint32_t b = uint32_t(2 * c - 1) & 0x3ffu;
+    const double bb = whole(b * b);
+    c -= c > 0 && bb * bb > t16;
     return c > 255 ? 255 : c;
 }
 
-// The largest of the wave's magnitudes by their bits: a NaN is the largest of all.
-__device__ __forceinline__ float wave_peak(uint32_t bits) {
-#pragma unroll
-    for (int off = 32; off > 0; off >>= 1) {
-        const uint32_t o = __shfl_xor(bits, off);
-        bits = o > bits ? o : bits;
+// The largest of the wave's magnitudes by their bits, by moves within the
+// register file: a NaN is the largest of all.
+template <int OFF> __device__ __forceinline__ uint32_t lane_max(uint32_t x) {
+    uint32_t a = x, b;
+    if constexpr (OFF == 16 || OFF == 32) {
+        const auto r = OFF == 16 ? __builtin_amdgcn_permlane16_swap(x, x, false, false)
+                                 : __builtin_amdgcn_permlane32_swap(x, x, false, false);
+        a = r[0], b = r[1];
+    } else {
+        // quad_perm [1,0,3,2] and [2,3,0,1], row_half_mirror, row_mirror
+        constexpr int ctrl = OFF == 1 ? 0xB1 : OFF == 2 ? 0x4E : OFF == 4 ? 0x141 : 0x140;
+        b = uint32_t(__builtin_amdgcn_update_dpp(0, int(x), ctrl, 0xf, 0xf, true));
     }
-    return __builtin_bit_cast(float, bits);
+    return a > b ? a : b;
+}
+__device__ __forceinline__ float wave_peak(uint32_t x) {
+    x = lane_max<1>(x), x = lane_max<2>(x), x = lane_max<4>(x), x = lane_max<8>(x);
+    x = lane_max<32>(lane_max<16>(x));
+    return __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(int(x)));
+}
+__device__ __forceinline__ double of_lane(double x, int lane) {
+    const uint64_t b = __builtin_bit_cast(uint64_t, x);
+    const uint32_t lo = uint32_t(__builtin_amdgcn_readlane(int(uint32_t(b)), lane)),
+                   hi = uint32_t(__builtin_amdgcn_readlane(int(uint32_t(b >> 32)), lane));
+    return __builtin_bit_cast(double, uint64_t(hi) << 32 | lo);
 }
 __device__ __forceinline__ uint32_t magnitude_bits(float x) { return __builtin_bit_cast(uint32_t, x) & 0x7fffffffu; }
 
@@ -357,10 +384,25 @@ __global__ __launch_bounds__(256) void k_adamw8(Table tab, Hyper hp, State* __re
     store4<f4>(e.p + i, p, left, wide);
     if (e.copy) store4<h4>(e.copy + i, h, left, wide);
     const float am = wave_peak(top_m), av = wave_peak(top_v);
-    const double inv_m = am > 0.f ? kTopM / double(am) : 0.0, inv_v = av > 0.f ? kTopV / double(av) : 0.0;
+    // one division for both: the even lanes' and the odd lanes'
+    const bool odd = threadIdx.x & 1;
+    const float a = odd ? av : am;
+    const double inv = a > 0.f ? (odd ? 16.0 * kTopV : 4.0 * kTopM) / double(a) : 0.0;
+    const double inv_m = of_lane(inv, 0), inv_v = of_lane(inv, 1);
+    // in 32 bits from products of 32 where none of them overflows
+    const bool plain = am > 0x1p-80f && av > 0x1p-80f && am < 0x1p80f && av < 0x1p80f;
+    const float near_m = float(inv_m), near_v = float(inv_v);
+    f4 nm, nv;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) nm[j] = fabsf(float(m[j])) * near_m, nv[j] = float(v[j]) * near_v;
+    if (!plain) {
+        asm volatile("");       // a branch: as selections both ways would be worked out
+#pragma unroll
+        for (int j = 0; j < 4; ++j) nm[j] = float(fabs(m[j]) * inv_m), nv[j] = float(v[j] * inv_v);
+    }
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-        const int cm = encode_m(fabs(m[j]) * inv_m), cv = encode_v(v[j] * inv_v);
+        const int cm = encode_m(fabs(m[j]) * inv_m, nm[j]), cv = encode_v(v[j] * inv_v, nv[j]);
         qm[j] = int8_t(m[j] < 0 ? -cm : cm);
         qv[j] = uint8_t(cv == 0 && v[j] > 0 ? 1 : cv);
     }
