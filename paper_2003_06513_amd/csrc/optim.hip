@@ -432,12 +432,13 @@ __global__ __launch_bounds__(256) void k_moments(const int8_t* __restrict__ qm, 
     store4<f4>(v + i, y, left, wide);
 }
 
-// ---- the norm.  No finite gradient's square overflows or vanishes: an fp32
-// one is squared in 64 bits; an fp16 one has an exact square in 32, of which
-// four are added there (two roundings, at most 2^-23 of their sum: a
-// conversion to 64 bits takes four times as long as another operation, and
-// with one for every element 64 x 512 x 512 x 9 took 164 us).  Sums in 64
-// bits; one partial sum per block, added in a fixed order.
+// ---- the norm.  Sums in 64 bits, one partial sum per block, added in a fixed
+// order; no finite gradient's square overflows or vanishes.  An fp32 one is
+// squared in 64 bits.  An fp16 one has an exact square in 32, whose bits, moved
+// up by 29, are those of a double 2^896 times smaller: a conversion takes as
+// long as four other operations, and with one for every element 64 x 512 x 512
+// x 9 took 164 us, not 51.  (Four squares added in 32 bits first, as fast, were
+// not exact enough: the clip factor's last bit decides codes of 8-bit moments.)
 __device__ __forceinline__ double block_sum(double x) {
     __shared__ double part[16];
 #pragma unroll
@@ -449,12 +450,27 @@ __device__ __forceinline__ double block_sum(double x) {
     return x;
 }
 
-__device__ __forceinline__ double squares(const f4& g, bool half, double acc) {
-    if (half) return acc + double(fmaf(g[1], g[1], g[0] * g[0]) + fmaf(g[3], g[3], g[2] * g[2]));
+struct Squares {
+    double sum = 0.0, tiny = 0.0;       // tiny: 2^-896 of the fp16 squares
+    float rough = 0.f;                  // of those, whether any is not finite: no sum of finite ones overflows
+    __device__ __forceinline__ void add(const f4& g, bool half) {
 #pragma unroll
-    for (int j = 0; j < 4; ++j) acc = fma(double(g[j]), double(g[j]), acc);
-    return acc;
-}
+        for (int j = 0; j < 4; ++j) {
+            if (half) {
+                const float q = g[j] * g[j];
+                const uint32_t b = __builtin_bit_cast(uint32_t, q);
+                tiny += __builtin_bit_cast(double, uint64_t(b) << 29);
+                rough += q;
+            } else {
+                sum = fma(double(g[j]), double(g[j]), sum);
+            }
+        }
+    }
+    __device__ __forceinline__ double all() const {
+        const double s = fma(tiny, 0x1p896, sum);
+        return __builtin_isfinite(rough) ? s : s + double(rough);
+    }
+};
 
 struct Clip {
     float scale, max_norm;
@@ -475,7 +491,7 @@ __device__ __forceinline__ void clip(const Clip& k, double squares) {
 constexpr int kAhead = 8;
 template <int THREADS>
 __global__ __launch_bounds__(THREADS) void k_norm_parts(GradTable tab, bool add, double* __restrict__ part, Clip alone) {
-    double acc = 0.0;
+    Squares acc;
     const uint32_t all = gridDim.x * (THREADS / 256), per = (tab.chunks + all - 1) / all;
     // the same for a whole wave, which the compiler has to know: 51 us, not 76, on 64 x 512 x 512 x 9 fp16
     uint32_t c = (blockIdx.x * (THREADS / 256) + uint32_t(__builtin_amdgcn_readfirstlane(int(threadIdx.x >> 8)))) * per;
@@ -492,24 +508,25 @@ __global__ __launch_bounds__(THREADS) void k_norm_parts(GradTable tab, bool add,
 #pragma unroll
                 for (int u = 0; u < kAhead; ++u) g[u] = *reinterpret_cast<const h4*>(static_cast<const uint16_t*>(e.g) + i + u * 1024);
 #pragma unroll
-                for (int u = 0; u < kAhead; ++u) acc = squares(widened(g[u]), true, acc);
+                for (int u = 0; u < kAhead; ++u) acc.add(widened(g[u]), true);
             } else {
                 f4 g[kAhead];
 #pragma unroll
                 for (int u = 0; u < kAhead; ++u) g[u] = *reinterpret_cast<const f4*>(static_cast<const float*>(e.g) + i + u * 1024);
 #pragma unroll
-                for (int u = 0; u < kAhead; ++u) acc = squares(g[u], false, acc);
+                for (int u = 0; u < kAhead; ++u) acc.add(g[u], false);
             }
             c += kAhead;
         } else {
-            if (i < e.numel) acc = squares(opened(load_grad<false>(e.g, i, e.numel - i < 4 ? int(e.numel - i) : 4, e.flags), e.flags), half, acc);
+            if (i < e.numel)
+                acc.add(opened(load_grad<false>(e.g, i, e.numel - i < 4 ? int(e.numel - i) : 4, e.flags), e.flags), half);
             ++c;
         }
     }
-    acc = block_sum(acc);
+    const double sum = block_sum(acc.all());
     if (threadIdx.x != 0) return;
-    if (alone.out) clip(alone, acc);
-    else part[blockIdx.x] = add ? part[blockIdx.x] + acc : acc;
+    if (alone.out) clip(alone, sum);
+    else part[blockIdx.x] = add ? part[blockIdx.x] + sum : sum;
 }
 
 __global__ __launch_bounds__(256) void k_norm_end(const double* __restrict__ part, int n, Clip k) {

@@ -73,6 +73,43 @@ def test_norm(sizes, half):
             assert np.abs(got - want).max() <= 2 * U32 * max(want), (got, want)
 
 
+@pytest.mark.parametrize("half", [False, True])
+def test_norm_rounds_once(half):
+    """Squares and sums in 64 bits (2^-53 of the sum each, far below 2^-10 of a
+    rounding of 32): norm and factor are those of 64 bits rounded once.  The
+    last bit of the factor decides codes of 8-bit moments."""
+    torch = torch_mod()
+    rng = np.random.default_rng(77)
+    out = torch.zeros(2, device="cuda")
+    most = float(np.float32(1e-3))      # the argument has 32 bits: 1e-3 itself is 4.7e-8 of it away
+    for k in list(range(1, 40)) + [100, 333, 1000, 5000, 20_000, 70_001] * 5:
+        g = (10.0 ** rng.uniform(-4, 2) * rng.standard_normal(k)).astype(np.float16 if half else np.float32)
+        if not g.any():
+            continue
+        note("norm of %d values" % k)
+        B.grad_norm(B.ParamList(None, [torch.from_numpy(g).cuda()]), out, max_norm=1e-3)
+        want = np.array(train.grad_norm([g], 1.0, most))
+        assert (np.abs(_h(out) - want) <= U32 * (1 + 2.0 ** -10) * want).all(), (k, _h(out), want)
+
+
+@pytest.mark.parametrize("bad", [np.inf, -np.inf, np.nan])
+def test_norm_of_half_precision_that_is_not_finite(bad):
+    torch = torch_mod()
+    out = torch.zeros(2, device="cuda")
+    for n, at in ((1, 0), (5000, 4999), (70000, 31), (70000, 69999)):
+        g = torch.full((n,), 65504.0, dtype=torch.float16, device="cuda")
+        B.grad_norm(B.ParamList(None, [g]), out)
+        assert abs(float(out[0]) / (65504 * np.sqrt(n)) - 1) < 1e-6 and float(out[1]) == 1.0
+        g[at] = bad
+        B.grad_norm(B.ParamList(None, [g]), out)
+        assert (np.isnan(_h(out)[0]) if np.isnan(bad) else _h(out)[0] == np.inf) and np.isnan(_h(out)[1])
+    least = torch.full((3,), 2.0 ** -24, dtype=torch.float16, device="cuda")
+    B.grad_norm(B.ParamList(None, [least]), out)
+    assert abs(float(out[0]) / (2.0 ** -24 * np.sqrt(3)) - 1) < 1e-6
+    B.grad_norm(B.ParamList(None, [torch.zeros(5000, dtype=torch.float16, device="cuda")]), out, max_norm=1.0)
+    assert np.array_equal(_h(out), [0, 1])
+
+
 def test_norm_extremes():
     torch = torch_mod()
     out = torch.zeros(2, device="cuda")
