@@ -335,8 +335,9 @@ psc_status psc_group_norm_bwd(int32_t dtype, int32_t layout, const void *d_x, co
  * norm of all their gradients.  The list is host memory, read before the call
  * returns; the addresses in it go to the kernels as arguments, so a captured
  * call replays on the same tensors.  Tensors need only the alignment of their
- * elements; 16 bytes (8 for fp16, 4 for 8-bit codes) is fastest.  No tensor
- * of a list may overlap another that the call writes. */
+ * elements (16 bytes, 8 for fp16, 4 for 8-bit codes is fastest) and the 48
+ * bits that this machine's addresses have.  No tensor of a list may overlap
+ * another that the call writes. */
 typedef struct psc_param {
     float *param;         /* [numel], updated in place */
     const void *grad;     /* [numel], grad_dtype */

@@ -624,7 +624,6 @@ hipError_t launch_adamw(const ParamView* q, int count, const AdamwArgs& a, const
             Entry e{};
             for (int k = 0; k < kAddresses; ++k) {
                 const uint64_t a = reinterpret_cast<uintptr_t>(at[k]);
-                if (a >> 48) return hipErrorInvalidDevicePointer;
                 e.lo[k] = uint32_t(a);
                 e.hi[k / 2] |= uint32_t(a >> 32) << (16 * (k & 1));
             }

@@ -658,6 +658,11 @@ static psc_status check_params(const psc_param* q, int32_t count, bool step) {
                                (q[i].state_bits == 32 ? reinterpret_cast<uintptr_t>(q[i].m) | reinterpret_cast<uintptr_t>(q[i].v) : 0);
         if ((four & 3u) || (reinterpret_cast<uintptr_t>(q[i].copy) & 1u))
             return fail(PSC_ERR_ARG, "params[%d]: a tensor is not aligned to its elements", i);
+        for (const void* p : {static_cast<const void*>(q[i].param), q[i].grad, static_cast<const void*>(q[i].copy),
+                              static_cast<const void*>(q[i].m), static_cast<const void*>(q[i].v),
+                              static_cast<const void*>(q[i].state_bits == 8 ? q[i].scale : nullptr)})
+            if (uint64_t(reinterpret_cast<uintptr_t>(p)) >> 48)
+                return fail(PSC_ERR_ARG, "params[%d]: an address has more than 48 bits", i);
     }
     return PSC_OK;
 }

@@ -93,6 +93,8 @@ def test_lists_are_refused(L, change, text):
     (dict(weight_decay=float("nan")), "weight_decay"), (dict(param=None), "non-NULL"), (dict(m=None), "non-NULL"),
     (dict(v=None), "non-NULL"), (dict(param=FAKE + 2), "aligned"), (dict(m=FAKE + 1), "aligned"),
     (dict(copy=FAKE + 1), "aligned"), (dict(state_bits=8, scale=None), "scale"), (dict(state_bits=8, scale=FAKE + 4), "scale"),
+    (dict(param=1 << 48), "48 bits"), (dict(grad=1 << 63), "48 bits"), (dict(copy=1 << 50), "48 bits"),
+    (dict(m=1 << 48), "48 bits"), (dict(v=1 << 48), "48 bits"), (dict(state_bits=8, scale=1 << 48), "48 bits"),
 ])
 def test_step_refuses_tensors(L, change, text):
     q, opt = (B.CParam * 1)(_param(**change)), B.CAdamW(0.1, 0.9, 0.99, 1e-8, None)
