@@ -226,13 +226,36 @@ __device__ __forceinline__ f4 opened(const f4& raw, uint32_t flags) {
     return widened(__builtin_bit_cast(h4, half));
 }
 
-// p from the new moments.  The quotient by v_rcp_f32 and v_sqrt_f32, each
-// within one unit in the last place: the step is at most a few 2^-23 of
-// itself off, far below the rounding of p.
-__device__ __forceinline__ float updated(float p, float m, float v, float decay, float rate, float root, float eps) {
-    const float d = fmaf(__builtin_amdgcn_sqrtf(v), root, eps);
+// sqrt(v) root + eps, by v_sqrt_f32, which is within one unit in the last place
+// but takes a v below 2^-126 for zero: a small one is scaled by 2^192 first (8
+// bits: in fp64, where codes far below their group's largest are less than
+// fp32's least).  A zero needs no scaling, and is common; of the others a wave
+// rarely has any.
+template <class T>
+__device__ __forceinline__ void denominators(const T (&v)[4], float root, float eps, float (&d)[4]) {
+    constexpr int up = sizeof(T) == 8 ? 192 : 96;
+    constexpr T least = T(0x1p-96);
+    bool small = false;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        d[j] = fmaf(__builtin_amdgcn_sqrtf(float(v[j])), root, eps);
+        small |= (v[j] < least) & (v[j] > T(0));
+    }
+    if (small) {
+        const T scale = up == 192 ? T(0x1p192) : T(0x1p96f);
+        const float less = root * (up == 192 ? 0x1p-96f : 0x1p-48f);
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (v[j] < least) d[j] = fmaf(__builtin_amdgcn_sqrtf(float(v[j] * scale)), less, eps);
+    }
+}
+// p from the new m and sqrt(v) / sqrt(1 - b2^t) + eps.  The quotient by
+// v_rcp_f32, which is within one unit in the last place (d is at least
+// FLT_MIN): the step is at most a few 2^-23 of itself off, far below the
+// rounding of p.  m by the reciprocal first: the rate times m may be subnormal.
+__device__ __forceinline__ float updated(float p, float m, float d, float decay, float rate) {
     const float q = fmaf(-decay, p, p);
-    return fmaf(-rate * m, __builtin_amdgcn_rcpf(d), q);
+    return fmaf(-rate, m * __builtin_amdgcn_rcpf(d), q);
 }
 
 // A step of nothing.
@@ -255,13 +278,19 @@ __global__ __launch_bounds__(256) void k_adamw32(Table tab, Hyper hp, State* __r
     if (!n.go) return;
     const f4 g = opened(raw, e.flags);
     const float decay = n.lr * e.wd;
-    h4 h;
+    float w[4], d[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
         const float gj = g[j] * n.factor;
         m[j] = fmaf(hp.b1, m[j], hp.c1 * gj);
-        v[j] = fmaf(hp.b2, v[j], hp.c2 * (gj * gj));
-        p[j] = updated(p[j], m[j], v[j], decay, n.rate, n.root, hp.eps);
+        w[j] = fmaf(hp.b2, v[j], hp.c2 * (gj * gj));
+    }
+    denominators(w, n.root, hp.eps, d);
+    h4 h;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        v[j] = w[j];
+        p[j] = updated(p[j], m[j], d[j], decay, n.rate);
         h[j] = Elt<DT_F16>::from_f(p[j]);
     }
     store4<f4>(e.p + i, p, left, wide);
@@ -373,7 +402,12 @@ __global__ __launch_bounds__(256) void k_adamw8(Table tab, Hyper hp, State* __re
         const double gj = g[j];
         m[j] = fma(power_m(qm[j]), km, gj * kg);
         v[j] = fma(power_v(qv[j]), kv, gj * gj * kgg);
-        p[j] = updated(p[j], float(m[j]), float(v[j]), decay, n.rate, n.root, hp.eps);
+    }
+    float d[4];
+    denominators(v, n.root, hp.eps, d);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        p[j] = updated(p[j], float(m[j]), d[j], decay, n.rate);
         h[j] = Elt<DT_F16>::from_f(p[j]);
         if (j < left) {
             const uint32_t bm = magnitude_bits(float(m[j])), bv = magnitude_bits(float(v[j]));

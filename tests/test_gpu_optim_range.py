@@ -1,0 +1,113 @@
+"""AdamW over the whole range of arguments that it accepts: eps down to
+FLT_MIN, betas from 0 to the last number below 1, moments and gradients at
+both ends of fp32.
+
+Bounds (u = 2^-24, s = 2^-150, half of the least subnormal).  m takes two
+products and a sum of rounded constants: 4 u of |b1 m| + |(1-b1) g| + 3 s.  v:
+5 u + 3 s.  The update is compared with the formula at the moments that the
+step left (32 bits: its own new m and v; 8 bits: the fp64 ones, rounded to
+fp32 on the way, 2 u + s each before the quotient), so that what is checked is
+the root and the quotient: lr / (1-b1^t) and 1 / sqrt(1-b2^t) take a logarithm
+rounded to fp32, a product, an exponential of at most two units in the last
+place and a division or a root and a reciprocal (8 u and 6 u), the root of v
+and the reciprocal one unit each (4 u), three more roundings: 21 u, with the
+rounded lr and eps 23 u; 24 u are allowed, and a rounding of the parameter."""
+import numpy as np
+import pytest
+
+from oracle import train
+from paper_2003_06513_amd import binding as B
+from gpu_cases import U32, dev, note, torch_mod
+
+pytestmark = pytest.mark.gpu
+SUB = 2.0 ** -150
+LEAST = float(np.finfo(np.float32).tiny)
+LAST = 1.0 - 2.0 ** -24         # the last fp32 below 1
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _need_gpu():
+    torch = pytest.importorskip("torch")
+    if not torch.cuda.is_available():
+        pytest.skip("no HIP device")
+    B.lib()
+
+
+def _f(x):
+    return float(np.float32(x))
+
+
+def _update(m, v, t, lr, b1, b2, eps):
+    """lr / (1 - b1^t) m / (sqrt(v / (1 - b2^t)) + eps) in fp64."""
+    return _f(lr) * (m / (1 - b1 ** t)) / (np.sqrt(v / (1 - b2 ** t)) + _f(eps))
+
+
+def _near(p, want, update, what, more=0.0):
+    bound = 24 * U32 * np.abs(update) + U32 * np.abs(want) + SUB + more
+    err = np.abs(p - want)
+    assert (err <= bound).all(), "%s: p off by %.3g bounds" % (what, (err / bound).max())
+
+
+@pytest.mark.parametrize("eps", [LEAST, 1e-30, 1e-20, 1e-12, 1e-8])
+@pytest.mark.parametrize("betas", [(0.9, 0.999), (0.0, 0.0), (0.0, 0.999), (0.5, 0.0), (0.99, LAST)])
+@pytest.mark.parametrize("shift", [0, 1])
+def test_small_second_moments(betas, eps, shift):
+    """Second moments from 0 and the least subnormal up, with parameters of 0 whose whole value is the update."""
+    torch = torch_mod()
+    rng = np.random.default_rng(5)
+    b1, b2 = (_f(b) for b in betas)
+    n, t, lr = 5000, 7, 1e-3
+    # the moment that a gradient's square leaves, or less, or nothing at all
+    g = (10.0 ** rng.uniform(-23, -6, n) * rng.choice([-1.0, 1.0], n)).astype(np.float32)
+    v0 = (g.astype(np.float64) ** 2 * 10.0 ** rng.uniform(-2, 2, n)).astype(np.float32)
+    m0 = (np.sqrt(v0.astype(np.float64)) * rng.uniform(-1, 1, n)).astype(np.float32)
+    v0[:64] = np.float32(2.0 ** -149) * np.arange(64)
+    g[:128], m0[:128] = 0, 1e-25
+    buf = torch.zeros(n + shift, device="cuda")
+    p = buf[shift:]
+    opt = B.AdamW([p], [dev(g)], lr=lr, betas=betas, eps=eps)
+    opt.m[:n], opt.v[:n] = dev(m0), dev(v0)
+    opt.steps.fill_(t - 1)
+    note("small second moments, betas %s eps %g" % (betas, eps))
+    opt.step()
+    torch.cuda.synchronize()
+    m, v, p = (x[:n].cpu().numpy().astype(np.float64) for x in (opt.m, opt.v, p))
+    _, rm, rv = train.adamw(np.zeros(n), g, m0, v0, t, lr, b1, b2, eps, 0.0)
+    g = np.abs(g.astype(np.float64))
+    assert (np.abs(m - rm) <= 4 * U32 * (b1 * np.abs(m0) + (1 - b1) * g) + 3 * SUB).all()
+    assert (np.abs(v - rv) <= 5 * U32 * rv + 3 * SUB).all()
+    assert ((v > 0) & (v < LEAST)).any() or b2 == 0
+    update = _update(m, v, t, lr, b1, b2, eps)
+    _near(p, -update, update, "eps %g" % eps)
+    assert int(opt.steps) == t
+
+
+@pytest.mark.parametrize("eps", [LEAST, 1e-30, 1e-20, 1e-8])
+@pytest.mark.parametrize("betas", [(0.9, 0.999), (0.0, 0.0), (0.0, 0.999), (0.5, 0.0), (0.99, LAST)])
+def test_small_second_moments_of_8_bits(betas, eps):
+    """Codes far below their group's largest stand for values that fp32 does not hold."""
+    torch = torch_mod()
+    rng = np.random.default_rng(6)
+    b1, b2 = (_f(b) for b in betas)
+    n, t, lr = 4096, 7, 1e-3
+    scale = np.stack([10.0 ** rng.uniform(-20, -15, n // 256), 10.0 ** rng.uniform(-37, -30, n // 256)], 1)
+    scale = scale.astype(np.float32)
+    # gradients that leave the groups' scales where they are, or about there
+    g = (10.0 ** rng.uniform(-26, -19, n) * rng.choice([-1.0, 1.0], n)).astype(np.float32)
+    g[rng.random(n) < 0.3] = 0
+    qm, qv = rng.integers(-127, 128, n).astype(np.int8), rng.integers(0, 256, n).astype(np.uint8)
+    few = rng.random(n) < 0.5
+    qv[few] = rng.integers(0, 4, int(few.sum()))
+    qm[::256], qv[::256] = 127, 255
+    p = torch.zeros(n, device="cuda")
+    opt = B.AdamW([p], [dev(g)], lr=lr, betas=betas, eps=eps, state_bits=8)
+    opt.m.copy_(dev(qm)), opt.v.copy_(dev(qv)), opt.scale.copy_(dev(scale))
+    opt.steps.fill_(t - 1)
+    note("small second moments of 8 bits, betas %s eps %g" % (betas, eps))
+    opt.step()
+    torch.cuda.synchronize()
+    _, rm, rv = train.adamw(np.zeros(n), g, train.decode_m(qm, scale), train.decode_v(qv, scale), t, lr, b1, b2, eps, 0.0)
+    update = _update(rm, rv, t, lr, b1, b2, eps)
+    from_m = SUB * lr / (1 - b1 ** t) / (np.sqrt(rv / (1 - b2 ** t)) + _f(eps))
+    _near(p.cpu().numpy().astype(np.float64), -update, update, "eps %g" % eps, 2 * U32 * np.abs(update) + from_m)
+    assert ((rv > 0) & (rv < 2.0 ** -149)).any() or b2 == 0
