@@ -390,7 +390,8 @@ psc_status psc_grad_norm(const psc_param *h_params, int32_t count, float scale, 
  * The step computes with what they stand for in fp64, updates the parameter
  * with the new moments before they are rounded, and rounds sqrt|m| and
  * v^(1/4) to the nearest code; v > 0 keeps a code above 0.  A gradient that is
- * not finite spoils the moments of its 256 elements (with 32 bits: its own). */
+ * not finite, or whose (1 - beta2) g^2 passes fp32, spoils the moments of its
+ * 256 elements (with 32 bits: its own). */
 #define PSC_ADAMW_STATE_BYTES 4352
 psc_status psc_adamw_step(const psc_param *h_params, int32_t count, const psc_adamw *opt,
                           const float *d_factor, void *d_state, void *stream);

@@ -283,7 +283,7 @@ __global__ __launch_bounds__(256) void k_adamw32(Table tab, Hyper hp, State* __r
     for (int j = 0; j < 4; ++j) {
         const float gj = g[j] * n.factor;
         m[j] = fmaf(hp.b1, m[j], hp.c1 * gj);
-        w[j] = fmaf(hp.b2, v[j], hp.c2 * (gj * gj));
+        w[j] = fmaf(hp.b2, v[j], hp.c2 * gj * gj);      // in this order: the square may pass fp32 where this does not
     }
     denominators(w, n.root, hp.eps, d);
     h4 h;

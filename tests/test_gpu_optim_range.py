@@ -111,3 +111,26 @@ def test_small_second_moments_of_8_bits(betas, eps):
     from_m = SUB * lr / (1 - b1 ** t) / (np.sqrt(rv / (1 - b2 ** t)) + _f(eps))
     _near(p.cpu().numpy().astype(np.float64), -update, update, "eps %g" % eps, 2 * U32 * np.abs(update) + from_m)
     assert ((rv > 0) & (rv < 2.0 ** -149)).any() or b2 == 0
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_large_gradients(bits):
+    """A gradient whose square passes fp32, while (1 - beta2) times it does not, is like any other."""
+    torch = torch_mod()
+    rng = np.random.default_rng(7)
+    n, lr = 1500, 1e-2
+    g = (10.0 ** rng.uniform(17, 20.6, n) * rng.choice([-1.0, 1.0], n)).astype(np.float32)
+    p = torch.zeros(n, device="cuda")
+    opt = B.AdamW([p], [dev(g)], lr=lr, state_bits=bits)
+    note("large gradients, %d bits" % bits)
+    opt.step()
+    m, v = opt.moments()
+    torch.cuda.synchronize()
+    _, rm, rv = train.adamw(np.zeros(n), g, np.zeros(n), np.zeros(n), 1, lr, 0.9, 0.999, 1e-8, 0.0)
+    update = _update(rm, rv, 1, lr, _f(0.9), _f(0.999), 1e-8)
+    # at the formula's own moments: 4 u of m, half of 5 u of v
+    _near(p.cpu().numpy().astype(np.float64), -update, update, "large", 7 * U32 * np.abs(update))
+    if bits == 32:
+        assert (np.abs(v[:n].cpu().numpy() - rv) <= 5 * U32 * rv).all()
+    else:
+        assert bool(torch.isfinite(v).all()) and bool(torch.isfinite(m).all())
