@@ -377,9 +377,10 @@ psc_status psc_grad_norm(const psc_param *h_params, int32_t count, float scale, 
  *   m = beta1 m + (1 - beta1) g,  v = beta2 v + (1 - beta2) g^2
  *   param = param - lr weight_decay param
  *           - lr / (1 - beta1^t) * m / (sqrt(v / (1 - beta2^t)) + eps)
- * If *d_factor is not finite nothing is changed and no step is counted.  With
- * 32 bits the moments are held in fp32: a gradient below 2^-75 / sqrt(1 - beta2)
- * leaves nothing in v, and the step divides by what v was and eps.
+ * If *d_factor or *opt->d_lr is not finite nothing is changed and no step is
+ * counted.  With 32 bits the moments are held in fp32: a gradient below 2^-75 /
+ * sqrt(1 - beta2) leaves nothing in v, and the step divides by what v was and
+ * eps.
  * d_state: PSC_ADAMW_STATE_BYTES bytes of the optimiser's, 256-byte aligned,
  * all zero before the first step; its first 8 bytes are the steps done
  * (int64).  Calls with one state must not overlap.

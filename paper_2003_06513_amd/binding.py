@@ -838,7 +838,8 @@ def adamw_step(params: ParamList, state, lr, betas=(0.9, 0.999), eps: float = 1e
     """psc_adamw_step: one step on every tensor of the list.  ``state``: a
     device tensor of ADAMW_STATE_BYTES bytes, zeros before the first step; ``lr``: a number,
     or an fp32 device tensor that the step reads; ``factor``: None, or an fp32
-    device tensor whose first element the gradients are multiplied by."""
+    device tensor whose first element the gradients are multiplied by.  One of
+    these that is not finite: no step."""
     on_device = hasattr(lr, "data_ptr")
     at = _same_device(params.one(), state, factor, lr if on_device else None)
     for t, name in ((factor, "factor"), (lr if on_device else None, "lr")):
@@ -917,7 +918,7 @@ class AdamW:
         return self._out
 
     def step(self, factor=None, stream=None):
-        """One step on every tensor (none if ``factor`` is not finite)."""
+        """One step on every tensor (none if ``factor`` or a learning rate on the device is not finite)."""
         self._hold(stream)
         adamw_step(self.params, self._state, self.lr, self.betas, self.eps, factor, stream)
 

@@ -126,14 +126,14 @@ __device__ __forceinline__ bool last_of(Line& line, uint32_t count) {
 // it out for the block.
 struct Now {
     float factor, rate, root, lr;
-    bool go;             // the factor is finite; else nothing is changed
+    bool go;             // the factor and the rate are finite; else nothing is changed
 };
 __device__ __forceinline__ Now now(const Hyper& hp, State* st, bool last) {
     __shared__ float both[2];
     Now n;
     n.factor = hp.factor ? *hp.factor : 1.f;
-    n.go = __builtin_isfinite(n.factor);
     n.lr = hp.d_lr ? *hp.d_lr : hp.lr;
+    n.go = __builtin_isfinite(n.factor) && __builtin_isfinite(n.lr);
     int64_t steps = 0;
     if (threadIdx.x < 64) {
         steps = st->steps;
@@ -259,8 +259,10 @@ __device__ __forceinline__ float updated(float p, float m, float d, float decay,
 }
 
 // A step of nothing.
-__global__ void k_adamw_none(const float* __restrict__ factor, State* __restrict__ st) {
-    if (!factor || __builtin_isfinite(*factor)) st->steps = st->steps + 1;
+__global__ void k_adamw_none(Hyper hp, State* __restrict__ st) {
+    if (hp.factor && !__builtin_isfinite(*hp.factor)) return;
+    if (hp.d_lr && !__builtin_isfinite(*hp.d_lr)) return;
+    st->steps = st->steps + 1;
 }
 
 // Four elements in a row per lane.
@@ -644,7 +646,7 @@ hipError_t launch_adamw(const ParamView* q, int count, const AdamwArgs& a, const
         else hipLaunchKernelGGL(k_adamw8, grid, dim3(256), 0, stream, tab, hp, st, last);
         clear(tab);
     };
-    if (left[0] + left[1] == 0) hipLaunchKernelGGL(k_adamw_none, dim3(1), dim3(1), 0, stream, factor, st);
+    if (left[0] + left[1] == 0) hipLaunchKernelGGL(k_adamw_none, dim3(1), dim3(1), 0, stream, hp, st);
     for (int bits : {32, 8}) {
         for (int i = 0; i < count; ++i) {
             if (q[i].state_bits != bits || q[i].numel == 0) continue;

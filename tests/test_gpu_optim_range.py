@@ -134,3 +134,31 @@ def test_large_gradients(bits):
         assert (np.abs(v[:n].cpu().numpy() - rv) <= 5 * U32 * rv).all()
     else:
         assert bool(torch.isfinite(v).all()) and bool(torch.isfinite(m).all())
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("bad", [np.inf, -np.inf, np.nan])
+def test_learning_rate_on_the_device_that_is_not_finite(bad, bits):
+    """Nothing is changed and no step counted, as with a factor that is not finite."""
+    torch = torch_mod()
+    rng = np.random.default_rng(8)
+    p, g = dev(rng.standard_normal(1000).astype(np.float32)), dev(rng.standard_normal(1000).astype(np.float32))
+    copy = torch.zeros(1000, dtype=torch.float16, device="cuda")
+    lr = torch.tensor([0.1], device="cuda")
+    opt = B.AdamW([p], [g], lr=lr, state_bits=bits, copies=[copy], weight_decay=0.1)
+    opt.step()
+    held = [t.clone() for t in (p, opt.m, opt.v, copy, opt.steps)]
+    lr.fill_(bad)
+    note("learning rate %s" % bad)
+    opt.step()
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(held, (p, opt.m, opt.v, copy, opt.steps)))
+    none = B.ParamList([], [], [], [])
+    B.adamw_step(none, opt._state, lr)
+    torch.cuda.synchronize()
+    assert int(opt.steps) == 1
+    lr.fill_(0.1)
+    opt.step()
+    B.adamw_step(none, opt._state, lr)
+    torch.cuda.synchronize()
+    assert int(opt.steps) == 3 and bool(torch.isfinite(p).all()) and not torch.equal(p, held[0])
