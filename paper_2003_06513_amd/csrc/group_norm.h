@@ -254,6 +254,15 @@ __device__ __forceinline__ void param_block(const Tail& t) {
     }
 }
 
+// mean and rstd as they are kept: both NaN where a value of the group is not
+// finite, or a sum passed fp32 (then the variance is not finite, whatever the
+// mean is).
+__device__ __forceinline__ float2 stats_of(float mu, float var, float eps) {
+    const bool fine = __builtin_isfinite(var);
+    const float nan = __builtin_nanf("");
+    return make_float2(fine ? mu : nan, fine ? 1.f / sqrtf(var + eps) : nan);
+}
+
 // The statistics of a group from its pieces, by a run of `lanes` lanes: the
 // means weighted by their counts, the squares about the common mean.
 __device__ __forceinline__ float2 joined_stats(const float4* p, int count, int lane, int lanes, float eps) {
@@ -269,7 +278,7 @@ __device__ __forceinline__ float2 joined_stats(const float4* p, int count, int l
         const float d = p[i].x - mu;
         sq += fmaf(p[i].z * d, d, p[i].y);
     }
-    return make_float2(mu, 1.f / sqrtf(run_sum(sq, lanes) / num + eps));
+    return stats_of(mu, run_sum(sq, lanes) / num, eps);
 }
 // S1 / M and S2 / M of the group whose channels begin with gamma[0].
 __device__ __forceinline__ float2 joined_back(const float2* p, int count, int pieces, const float* gamma, float m, int lane,

@@ -30,8 +30,8 @@ __global__ __launch_bounds__(1024) void k_gn_combine_fwd(const float4* __restric
     }
     sq = block_sum(sq, again);
     if (threadIdx.x == 0) {
-        mean[blockIdx.x] = mu;
-        rstd[blockIdx.x] = 1.f / sqrtf(sq / both.x + eps);
+        const float2 ms = stats_of(mu, sq / both.x, eps);
+        mean[blockIdx.x] = ms.x, rstd[blockIdx.x] = ms.y;
     }
 }
 

@@ -127,10 +127,7 @@ __global__ __launch_bounds__(threads_of(DT, V, K)) void k_gn_cols_fwd(const type
     __syncthreads();
     for (int k = threadIdx.x; k < p.width; k += blockDim.x) ch[k] = sum_of_channel(lds, q, k);
     __syncthreads();
-    each_group(q, count, ch, nullptr, [&](int g, float sum) {
-        gr[g] = sum / m;
-        if (mean) mean[g0 + g] = sum / m;
-    });
+    each_group(q, count, ch, nullptr, [&](int g, float sum) { gr[g] = sum / m; });
     __syncthreads();
     int g[V];
 #pragma unroll
@@ -153,9 +150,9 @@ __global__ __launch_bounds__(threads_of(DT, V, K)) void k_gn_cols_fwd(const type
     for (int k = threadIdx.x; k < p.width; k += blockDim.x) ch[k] = sum_of_channel(lds, q, k);
     __syncthreads();
     each_group(q, count, ch, nullptr, [&](int g, float sum) {
-        const float rs = 1.f / sqrtf(sum / m + eps);
-        gr[g] = rs;
-        if (rstd) rstd[g0 + g] = rs;
+        const float2 ms = stats_of(gr[g], sum / m, eps);
+        gr[g] = ms.y;
+        if (mean) mean[g0 + g] = ms.x, rstd[g0 + g] = ms.y;
     });
     __syncthreads();
 #pragma unroll

@@ -71,11 +71,9 @@ __global__ __launch_bounds__(threads_of(DT, V, K)) void k_gn_rows_fwd(const type
         }
         sq += on ? t : 0.f;
     }, Nothing());
-    k.r = 1.f / sqrtf(block_sum(sq, part + 16) / m + eps);
-    if (threadIdx.x == 0 && mean) {
-        mean[blockIdx.x] = k.mu;
-        rstd[blockIdx.x] = k.r;
-    }
+    const float2 ms = stats_of(k.mu, block_sum(sq, part + 16) / m, eps);
+    k.r = ms.y;
+    if (threadIdx.x == 0 && mean) mean[blockIdx.x] = ms.x, rstd[blockIdx.x] = ms.y;
     if (blockDim.x == 64) __syncthreads();      // the sums of larger blocks had one
     each<V, MASK, K>(s, b, [&](int i, int row, const Window& w, bool on) {
         const float2 gb = row_params[row];
