@@ -8,6 +8,7 @@
 #include <cstdio>
 #include <cstddef>
 #include <cstring>
+#include <initializer_list>
 #include <limits>
 #include <string>
 
@@ -575,6 +576,14 @@ static psc_status check_ws(const char* what, size_t need, const void* d_ws, size
     return PSC_OK;
 }
 
+// fp32 values that are read or written one by one: an address that is not a
+// multiple of 4 would be rounded down by a load that a whole wave has in common.
+static psc_status check_f32(const char* what, std::initializer_list<const void*> ptrs) {
+    for (const void* p : ptrs)
+        if (reinterpret_cast<uintptr_t>(p) & 3u) return fail(PSC_ERR_ARG, "%s is not aligned to its fp32 values", what);
+    return PSC_OK;
+}
+
 psc_status psc_group_norm_workspace(int32_t dtype, int32_t layout, int32_t n, int32_t c, int32_t h, int32_t w,
                                     int32_t groups, int32_t backward, int32_t aligned, size_t* bytes) {
     psc::GroupNormArgs a;
@@ -598,6 +607,7 @@ psc_status psc_group_norm_fwd(int32_t dtype, int32_t layout, const void* d_x, in
     if (overlaps(d_x, bytes, d_y, bytes)) return fail(PSC_ERR_ARG, "d_y overlaps d_x");
     const uintptr_t bits = reinterpret_cast<uintptr_t>(d_x) | reinterpret_cast<uintptr_t>(d_y);
     if (bits & (elt_size(dtype) - 1)) return fail(PSC_ERR_ARG, "d_x or d_y is not aligned to its elements");
+    if (psc_status s = check_f32("d_gamma, d_beta, d_mean or d_rstd", {d_gamma, d_beta, d_mean, d_rstd})) return s;
     if (psc_status s = check_ws("psc_group_norm_fwd", psc::group_norm_workspace_bytes(a, false, (bits & 15u) == 0), d_ws,
                                 ws_bytes))
         return s;
@@ -619,6 +629,9 @@ psc_status psc_group_norm_bwd(int32_t dtype, int32_t layout, const void* d_x, co
         return fail(PSC_ERR_ARG, "d_dx overlaps d_x or d_dy");
     const uintptr_t bits = reinterpret_cast<uintptr_t>(d_x) | reinterpret_cast<uintptr_t>(d_dy) | reinterpret_cast<uintptr_t>(d_dx);
     if (bits & (elt_size(dtype) - 1)) return fail(PSC_ERR_ARG, "d_x, d_dy or d_dx is not aligned to its elements");
+    if (psc_status s = check_f32("d_gamma, d_beta, d_mean, d_rstd, d_dgamma or d_dbeta",
+                                 {d_gamma, d_beta, d_mean, d_rstd, d_dgamma, d_dbeta}))
+        return s;
     if (psc_status s = check_ws("psc_group_norm_bwd", psc::group_norm_workspace_bytes(a, true, (bits & 15u) == 0), d_ws,
                                 ws_bytes))
         return s;
@@ -673,6 +686,7 @@ psc_status psc_grad_norm(const psc_param* h_params, int32_t count, float scale, 
     if (!(scale > 0.f) || !std::isfinite(scale)) return fail(PSC_ERR_ARG, "scale must be positive and finite");
     if (!(max_norm > 0.f)) return fail(PSC_ERR_ARG, "max_norm must be positive");
     if (!d_out) return fail(PSC_ERR_ARG, "d_out is NULL");
+    if (psc_status s = check_f32("d_out", {d_out})) return s;
     if (psc_status s = check_ws("psc_grad_norm", psc::grad_norm_workspace_bytes(), d_ws, ws_bytes)) return s;
     return device_status(psc::launch_grad_norm(reinterpret_cast<const psc::ParamView*>(h_params), count, scale, max_norm,
                                                d_out, d_ws, as_stream(stream)),
@@ -690,6 +704,7 @@ psc_status psc_adamw_step(const psc_param* h_params, int32_t count, const psc_ad
         return fail(PSC_ERR_ARG, "eps must be finite and at least FLT_MIN");
     if (!d_state || (reinterpret_cast<uintptr_t>(d_state) & 255u))
         return fail(PSC_ERR_ARG, "d_state must be non-NULL and 256-byte aligned");
+    if (psc_status s = check_f32("d_factor or d_lr", {d_factor, opt->d_lr})) return s;
     const psc::AdamwArgs a{opt->lr, opt->beta1, opt->beta2, opt->eps, opt->d_lr};
     return device_status(psc::launch_adamw(reinterpret_cast<const psc::ParamView*>(h_params), count, a, d_factor, d_state,
                                            as_stream(stream)),
@@ -702,6 +717,7 @@ psc_status psc_adamw_moments(const void* d_m, const void* d_v, const float* d_sc
     if (numel == 0) return ok();
     if (!d_m || !d_v || !d_scale || !d_m_out || !d_v_out) return fail(PSC_ERR_ARG, "every pointer must be non-NULL");
     if (reinterpret_cast<uintptr_t>(d_scale) & 7u) return fail(PSC_ERR_ARG, "d_scale must be 8-byte aligned");
+    if (psc_status s = check_f32("d_m_out or d_v_out", {d_m_out, d_v_out})) return s;
     return device_status(psc::launch_moments(static_cast<const int8_t*>(d_m), static_cast<const uint8_t*>(d_v), d_scale,
                                              numel, d_m_out, d_v_out, as_stream(stream)),
                          "psc_adamw_moments launch");

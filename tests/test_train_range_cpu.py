@@ -1,0 +1,35 @@
+"""Refusals of the group-normalisation and optimiser entry points at the ends of
+what they accept (CPU: every call fails before any HIP call)."""
+import ctypes
+
+import pytest
+
+from paper_2003_06513_amd import binding as B
+from test_train_abi_cpu import BWD, FAKE, FWD, _param, _says
+
+
+@pytest.fixture(scope="module")
+def L():
+    return B.lib()
+
+
+@pytest.mark.parametrize("name", ["gamma", "beta", "mean", "rstd", "dgamma", "dbeta"])
+@pytest.mark.parametrize("off", [1, 2, 3])
+def test_norm_parameters_and_statistics_that_are_not_aligned(L, name, off):
+    """A load that a wave has in common rounds such an address down: it would read other values."""
+    if name in FWD:
+        args = {**FWD, "mean": FAKE, "rstd": FAKE, name: FAKE + off}
+        _says(L.psc_group_norm_fwd(*args.values()), B.PSC_ERR_ARG, "aligned")
+    _says(L.psc_group_norm_bwd(*{**BWD, name: FAKE + off}.values()), B.PSC_ERR_ARG, "aligned")
+
+
+@pytest.mark.parametrize("off", [1, 2, 3])
+def test_optimiser_values_that_are_not_aligned(L, off):
+    q, bad = (B.CParam * 1)(_param()), FAKE + off
+    _says(L.psc_grad_norm(q, 1, 1.0, 1.0, bad, FAKE, 8192, None), B.PSC_ERR_ARG, "aligned")
+    opt = B.CAdamW(0.1, 0.9, 0.99, 1e-8, None)
+    _says(L.psc_adamw_step(q, 1, ctypes.byref(opt), bad, FAKE, None), B.PSC_ERR_ARG, "aligned")
+    opt = B.CAdamW(0.1, 0.9, 0.99, 1e-8, bad)
+    _says(L.psc_adamw_step(q, 1, ctypes.byref(opt), None, FAKE, None), B.PSC_ERR_ARG, "aligned")
+    for m_out, v_out in ((bad, FAKE), (FAKE, bad)):
+        _says(L.psc_adamw_moments(FAKE, FAKE, FAKE, 5, m_out, v_out, None), B.PSC_ERR_ARG, "aligned")
