@@ -307,10 +307,10 @@ psc_status psc_group_norm_workspace(int32_t dtype, int32_t layout, int32_t n, in
 
 /* d_y = act(u).  d_gamma and d_beta [c] may be NULL (1 and 0).  d_mean and
  * d_rstd [n][groups] receive the statistics that the backward reads; both may
- * be NULL.  groups divides c; eps is positive and finite.  d_y must not
- * overlap d_x.  n == 0 is a no-op.  A group with a value that is not finite,
- * or whose sum of x or of (x - mean)^2 passes fp32, has NaN statistics and
- * outputs; other groups are not touched by it. */
+ * be NULL.  groups divides c; eps is finite and at least FLT_MIN (fp32 loses
+ * squares below it).  d_y must not overlap d_x.  n == 0 is a no-op.  A group
+ * with a value that is not finite, or whose sum of x or of (x - mean)^2 passes
+ * fp32, has NaN statistics and outputs; other groups are not touched by it. */
 psc_status psc_group_norm_fwd(int32_t dtype, int32_t layout, const void *d_x, int32_t n, int32_t c,
                               int32_t h, int32_t w, int32_t groups, const float *d_gamma,
                               const float *d_beta, float eps, int32_t act, void *d_y, float *d_mean,

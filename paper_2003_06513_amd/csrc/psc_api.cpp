@@ -599,7 +599,8 @@ psc_status psc_group_norm_fwd(int32_t dtype, int32_t layout, const void* d_x, in
                               void* stream) {
     psc::GroupNormArgs a;
     if (psc_status s = check_group_norm(dtype, layout, n, c, h, w, groups, act, &a)) return s;
-    if (!(eps > 0.f) || !std::isfinite(eps)) return fail(PSC_ERR_ARG, "eps must be positive and finite");
+    if (!(eps >= std::numeric_limits<float>::min()) || !std::isfinite(eps))
+        return fail(PSC_ERR_ARG, "eps must be finite and at least FLT_MIN");
     if (!d_mean != !d_rstd) return fail(PSC_ERR_ARG, "d_mean and d_rstd must be both NULL or both non-NULL");
     if (n == 0) return ok();
     if (!d_x || !d_y) return fail(PSC_ERR_ARG, "d_x and d_y must be non-NULL");

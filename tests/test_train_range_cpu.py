@@ -33,3 +33,9 @@ def test_optimiser_values_that_are_not_aligned(L, off):
     _says(L.psc_adamw_step(q, 1, ctypes.byref(opt), None, FAKE, None), B.PSC_ERR_ARG, "aligned")
     for m_out, v_out in ((bad, FAKE), (FAKE, bad)):
         _says(L.psc_adamw_moments(FAKE, FAKE, FAKE, 5, m_out, v_out, None), B.PSC_ERR_ARG, "aligned")
+
+
+@pytest.mark.parametrize("eps", [1e-45, 1e-40, 1.1754942e-38])
+def test_eps_of_the_norm_below_the_least_normal(L, eps):
+    """Squares of about eps would be lost in fp32: rstd would be that of a group without spread."""
+    _says(L.psc_group_norm_fwd(*{**FWD, "eps": eps}.values()), B.PSC_ERR_ARG, "eps")
