@@ -3,6 +3,7 @@ what they accept (CPU: every call fails before any HIP call)."""
 import ctypes
 
 import pytest
+import torch
 
 from paper_2003_06513_amd import binding as B
 from test_train_abi_cpu import BWD, FAKE, FWD, _param, _says
@@ -39,3 +40,16 @@ def test_optimiser_values_that_are_not_aligned(L, off):
 def test_eps_of_the_norm_below_the_least_normal(L, eps):
     """Squares of about eps would be lost in fp32: rstd would be that of a group without spread."""
     _says(L.psc_group_norm_fwd(*{**FWD, "eps": eps}.values()), B.PSC_ERR_ARG, "eps")
+
+
+def test_current_stream_without_the_short_way(monkeypatch):
+    """A torch that lacks the entry point for a stream's bare handle has the same streams by its public ones."""
+    class Stream:
+        cuda_stream = 1234
+
+    monkeypatch.delattr(torch._C, "_cuda_getCurrentRawStream", raising=False)
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda device=None: Stream)
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 3)
+    for name in ("_TORCH", "_CURRENT"):
+        monkeypatch.setattr(B, name, None)
+    assert B._stream(None) == B._stream(None, 0) == B._stream(Stream) == 1234
