@@ -389,9 +389,10 @@ psc_status psc_grad_norm(const psc_param *h_params, int32_t count, float scale, 
  * With state_bits 8 the moments of 256 elements in a row share two scales,
  * their largest |m| and largest v: m's code q in -127..127 stands for
  * sign(q) (q / 127)^2 scale[0], v's code in 0..255 for (c / 255)^4 scale[1].
- * The step computes with what they stand for in fp64, updates the parameter
- * with the new moments before they are rounded, and rounds sqrt|m| and
- * v^(1/4) to the nearest code; v > 0 keeps a code above 0.  A gradient that is
+ * The new moments are computed in fp64 from what the codes stand for.  The
+ * parameter's update takes them before they become codes, in fp32 (m rounded
+ * to it; sqrt(v) of the fp64 value, to fp32's precision).  sqrt|m| and v^(1/4)
+ * are rounded to the nearest code; v > 0 keeps a code above 0.  A gradient that is
  * not finite, or whose (1 - beta2) g^2 passes fp32, spoils the moments of its
  * 256 elements (with 32 bits: its own). */
 #define PSC_ADAMW_STATE_BYTES 4352
