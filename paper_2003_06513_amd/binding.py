@@ -903,15 +903,20 @@ class AdamW:
         self._out = torch.zeros(2, dtype=torch.float32, device=device)
         self.norm, self.factor = self._out[:1], self._out[1:]
         self._ws = torch.empty(GRAD_NORM_WS_BYTES, dtype=torch.uint8, device=device)
+        self._at = self._state.get_device()
+        self._home = _stream(None, self._at)        # the stream whose pool all of this came from
 
     def _hold(self, stream):
-        """Work on another stream than the one that the memory came from: it is
-        not given out again before that is done."""
-        if stream is not None:
-            s = _torch_stream(stream)
-            for t in (self.m, self.v, self.scale, self._state, self._out, self._ws):
-                if t is not None:
-                    t.record_stream(s)
+        """Work on another stream than the one that the memory came from, be it
+        the current one or named: it is not given out again before that is
+        done.  (Work that is captured runs when and where it is replayed.)"""
+        if stream is None:
+            if _stream(None, self._at) == self._home or _torch().cuda.is_current_stream_capturing():
+                return
+        s = _torch_stream(stream)
+        for t in (self.m, self.v, self.scale, self._state, self._out, self._ws):
+            if t is not None:
+                t.record_stream(s)
 
     def grad_norm(self, max_norm: float = float("inf"), scale: float = 1.0, stream=None):
         """The norm of the gradients and the factor that clips them, which

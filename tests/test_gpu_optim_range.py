@@ -162,3 +162,26 @@ def test_learning_rate_on_the_device_that_is_not_finite(bad, bits):
     B.adamw_step(none, opt._state, lr)
     torch.cuda.synchronize()
     assert int(opt.steps) == 3 and bool(torch.isfinite(p).all()) and not torch.equal(p, held[0])
+
+
+def test_current_stream_that_is_not_the_buffers_own():
+    """Steps under another current stream, the optimiser dropped at once: its memory is not given out before they are
+    done, and they are done right."""
+    torch = torch_mod()
+    rng = np.random.default_rng(9)
+    p0, g0 = rng.standard_normal(300_000).astype(np.float32), rng.standard_normal(300_000).astype(np.float32)
+    want, p, g = dev(p0), dev(p0), dev(g0)
+    B.AdamW([want], [g], lr=0.1).step()
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    note("step on another current stream")
+    opt = B.AdamW([p], [g], lr=0.1)
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        for _ in range(3):
+            opt.grad_norm(1.0)
+        opt.step()
+    del opt
+    others = [torch.full((300_000,), 7.0, device="cuda") for _ in range(4)]
+    torch.cuda.synchronize()
+    assert torch.equal(p, want) and all(bool((t == 7).all()) for t in others)

@@ -53,3 +53,31 @@ def test_current_stream_without_the_short_way(monkeypatch):
     for name in ("_TORCH", "_CURRENT"):
         monkeypatch.setattr(B, name, None)
     assert B._stream(None) == B._stream(None, 0) == B._stream(Stream) == 1234
+
+
+def test_optimiser_memory_is_held_for_the_stream_that_works_on_it(monkeypatch):
+    """Also where that stream is the current one, not named: dropped early, the buffers would be given out while
+    its step still writes them."""
+    held = []
+
+    class Buffer:
+        def record_stream(self, s):
+            held.append(s)
+
+    opt = B.AdamW.__new__(B.AdamW)
+    opt.m, opt.v, opt.scale, opt._state, opt._out, opt._ws = Buffer(), Buffer(), None, Buffer(), Buffer(), Buffer()
+    opt._at, opt._home = 0, 10
+    now, capturing = [10], [False]
+    monkeypatch.setattr(B, "_stream", lambda stream, device=None: now[0] if stream is None else stream.cuda_stream)
+    monkeypatch.setattr(B, "_torch_stream", lambda stream: now[0] if stream is None else stream)
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: capturing[0])
+    opt._hold(None)
+    assert held == []
+    now[0] = 11
+    opt._hold(None)
+    assert held == [11] * 5
+    capturing[0] = True
+    opt._hold(None)
+    assert held == [11] * 5
+    opt._hold(12)
+    assert held[5:] == [12] * 5
