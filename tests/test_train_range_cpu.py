@@ -47,11 +47,13 @@ def test_current_stream_without_the_short_way(monkeypatch):
     class Stream:
         cuda_stream = 1234
 
-    monkeypatch.delattr(torch._C, "_cuda_getCurrentRawStream", raising=False)
+    for name in ("_cuda_getCurrentRawStream", "_cuda_getDevice"):
+        monkeypatch.delattr(torch._C, name, raising=False)
     monkeypatch.setattr(torch.cuda, "current_stream", lambda device=None: Stream)
     monkeypatch.setattr(torch.cuda, "current_device", lambda: 3)
-    for name in ("_TORCH", "_CURRENT"):
+    for name in ("_TORCH", "_CURRENT", "_DEVICE"):
         monkeypatch.setattr(B, name, None)
+    assert B._same_device() == 3
     assert B._stream(None) == B._stream(None, 0) == B._stream(Stream) == 1234
 
 
@@ -68,7 +70,8 @@ def test_optimiser_memory_is_held_for_the_stream_that_works_on_it(monkeypatch):
     opt.m, opt.v, opt.scale, opt._state, opt._out, opt._ws = Buffer(), Buffer(), None, Buffer(), Buffer(), Buffer()
     opt._at, opt._home = 0, 10
     now, capturing = [10], [False]
-    monkeypatch.setattr(B, "_stream", lambda stream, device=None: now[0] if stream is None else stream.cuda_stream)
+    B._torch()
+    monkeypatch.setattr(B, "_CURRENT", lambda device: now[0])
     monkeypatch.setattr(B, "_torch_stream", lambda stream: now[0] if stream is None else stream)
     monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: capturing[0])
     opt._hold(None)
