@@ -392,7 +392,8 @@ psc_status psc_grad_norm(const psc_param *h_params, int32_t count, float scale, 
  * The new moments are computed in fp64 from what the codes stand for.  The
  * parameter's update takes them before they become codes, in fp32 (m rounded
  * to it; sqrt(v) of the fp64 value, to fp32's precision).  sqrt|m| and v^(1/4)
- * are rounded to the nearest code; v > 0 keeps a code above 0.  A gradient that is
+ * are rounded to the nearest code, from the middle between two to the larger;
+ * v > 0 keeps a code above 0.  A gradient that is
  * not finite, or whose (1 - beta2) g^2 passes fp32, spoils the moments of its
  * 256 elements (with 32 bits: its own). */
 #define PSC_ADAMW_STATE_BYTES 4352

@@ -309,10 +309,13 @@ __global__ __launch_bounds__(256) void k_adamw32(Table tab, Hyper hp, State* __r
 // sqrt(v), which the step divides by, moves by 2/c of itself from code to
 // code, m likewise.  The code of x is the number of borders (k - 1/2)^2 (or
 // ^4) at or below x 127^2 / a (x 255^4 / a), taken in 64 bits, which this
-// machine multiplies as fast as 32: the borders are exact there, so that the
-// codes are those of the formula.  A v above zero keeps a code above zero:
-// with code 0 the next step would divide by eps alone.
+// machine multiplies as fast as 32.  The borders are exact there; the product
+// has two roundings, and is raised by more than those (2^-50 of itself), so
+// that an x on a border, as gradients of few bits and betas of 0 or 1/2 put
+// one, has the code above it.  A v above zero keeps a code above zero: with
+// code 0 the next step would divide by eps alone.
 constexpr double kTopM = 127.0 * 127.0, kTopV = 255.0 * 255.0 * 255.0 * 255.0;
+constexpr double kRaise = 1.0 + 0x1p-50;
 
 // Whole numbers in 64 bits: laid behind the exponent of 2^52 and that taken
 // away.  A conversion takes as long as four such operations; with them, the
@@ -329,7 +332,7 @@ __device__ __forceinline__ double power_v(uint32_t c) {
     const uint32_t s = c * c;
     return whole(s * s);
 }
-// Codes from 4 |m| 127^2 / a and 16 v 255^4 / a, and these in 32 bits.  The
+// Codes from 4 |m| 127^2 / a and 16 v 255^4 / a (raised), and these in 32 bits.  The
 // root is raised by more than its error, so that the code is right or one too
 // high; one look at the border below, (2 c - 1)^2 or ^4, tells which.
 __device__ __forceinline__ int encode_m(double t4, float near) {
@@ -423,7 +426,7 @@ __global__ __launch_bounds__(256) void k_adamw8(Table tab, Hyper hp, State* __re
     // one division for both: the even lanes' and the odd lanes'
     const bool odd = threadIdx.x & 1;
     const float a = odd ? av : am;
-    const double inv = a > 0.f ? (odd ? 16.0 * kTopV : 4.0 * kTopM) / double(a) : 0.0;
+    const double inv = a > 0.f ? (odd ? 16.0 * kRaise * kTopV : 4.0 * kRaise * kTopM) / double(a) : 0.0;
     const double inv_m = of_lane(inv, 0), inv_v = of_lane(inv, 1);
     // in 32 bits from products of 32 where none of them overflows
     const bool plain = am > 0x1p-80f && av > 0x1p-80f && am < 0x1p80f && av < 0x1p80f;

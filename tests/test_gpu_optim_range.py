@@ -185,3 +185,33 @@ def test_current_stream_that_is_not_the_buffers_own():
     others = [torch.full((300_000,), 7.0, device="cuda") for _ in range(4)]
     torch.cuda.synchronize()
     assert torch.equal(p, want) and all(bool((t == 7).all()) for t in others)
+
+
+def _codes_of_whole_numbers(x, peak, top, power):
+    """How many borders (k - 1/2)^power, k = 1 .. top, lie at or below x top^power / peak, in whole numbers."""
+    borders = (2 * np.arange(1, top + 1) - 1) ** power * peak
+    return np.searchsorted(borders, x * (2 * top) ** power, side="right")
+
+
+@pytest.mark.parametrize("half", [False, True])
+@pytest.mark.parametrize("unit", [1.0, 2.0 ** -7, 2.0 ** 5])
+def test_codes_of_values_on_borders(unit, half):
+    """Whole gradients and betas of 0: m and v are they and their squares, and many lie on a border between two codes
+    (1/4 of the largest m; 1/16, 1/1296 or 1/10000 of the largest v), where the code is the upper one."""
+    torch = torch_mod()
+    peaks = np.concatenate([np.arange(4, 1204, 4), [100 * k for k in range(1, 13)], [36 * k for k in range(1, 30)]])
+    g = np.stack([np.linspace(0, k, 256).astype(np.int64) for k in peaks])
+    g[:, 1], g[:, 2], g[:, 3] = peaks // 4, peaks // 10, peaks // 6
+    sign = np.where(np.arange(g.size) % 3 == 1, -1, 1)
+    p = torch.zeros(g.size, device="cuda")
+    grad = dev((unit * sign * g.reshape(-1)).astype(np.float16 if half else np.float32))
+    opt = B.AdamW([p], [grad], betas=(0.0, 0.0), state_bits=8)
+    note("codes on borders, unit %g" % unit)
+    opt.step()
+    torch.cuda.synchronize()
+    m = np.stack([_codes_of_whole_numbers(r, k, 127, 2) for r, k in zip(g, peaks)])
+    v = np.stack([np.maximum(_codes_of_whole_numbers(r * r, k * k, 255, 4), r > 0) for r, k in zip(g, peaks)])
+    assert np.array_equal(opt.m.cpu().numpy(), sign * m.reshape(-1))
+    assert np.array_equal(opt.v.cpu().numpy(), v.reshape(-1))
+    assert (4 * g == peaks[:, None]).sum() >= 300 and (10 * g == peaks[:, None]).sum() > 10 and \
+        (6 * g == peaks[:, None]).sum() > 10
