@@ -263,21 +263,29 @@ __device__ __forceinline__ float2 stats_of(float mu, float var, float eps) {
     return make_float2(fine ? mu : nan, fine ? 1.f / sqrtf(var + eps) : nan);
 }
 
-// The statistics of a group from its pieces, by a run of `lanes` lanes: the
-// means weighted by their counts, the squares about the common mean.
+// A piece in the sums of its group: mean x (rounded, and w what that lacks of
+// the true one), squares y about x, count z.  Its part of the sum, and of the
+// squares about mu.  Without w the rounding of x, which is of the size of the
+// values, not of their spread, would count once for every piece's distance
+// from the others: 10^4 spreads from zero rstd was 6e-5 off.
+__device__ __forceinline__ float sum_with(const float4& p, float sum) { return fmaf(p.z, p.x, fmaf(p.z, p.w, sum)); }
+__device__ __forceinline__ float squares_about(const float4& p, float mu) {
+    const float d = p.x - mu;
+    return fmaf(p.z * d, fmaf(2.f, p.w, d), p.y);
+}
+
+// The statistics of a group from its pieces, by a run of `lanes` lanes.
 __device__ __forceinline__ float2 joined_stats(const float4* p, int count, int lane, int lanes, float eps) {
     float sum = 0.f, num = 0.f;
     for (int i = lane; i < count; i += lanes) {
-        sum = fmaf(p[i].z, p[i].x, sum);
-        num += p[i].z;
+        const float4 t = p[i];
+        sum = sum_with(t, sum);
+        num += t.z;
     }
     num = run_sum(num, lanes);
     const float mu = run_sum(sum, lanes) / num;
     float sq = 0.f;
-    for (int i = lane; i < count; i += lanes) {
-        const float d = p[i].x - mu;
-        sq += fmaf(p[i].z * d, d, p[i].y);
-    }
+    for (int i = lane; i < count; i += lanes) sq += squares_about(p[i], mu);
     return stats_of(mu, run_sum(sq, lanes) / num, eps);
 }
 // S1 / M and S2 / M of the group whose channels begin with gamma[0].
@@ -413,28 +421,35 @@ struct Cols {
 // k / cg for k, cg < 2^16 (cg_m is at most cg - 1 too large: less than 2^32 / cg in the product); cg == 1: 0.
 __device__ __forceinline__ int group_of(const Cols& q, int k) { return q.cg_m ? int(__umulhi(uint32_t(k), q.cg_m)) : k; }
 
-// Adds s[V] of each thread over the threads of the wave that have the same
-// channels, and leaves the wave's sums in `buf`, of which there are
-// sum_rows(q) rows of `tile`.
+// Adds s[N] of each thread over the threads of the wave that have the same
+// channels: the lanes of a row of 16 by turning it, which keeps the columns
+// below the turn apart.  Several sums go together, step by step: each step of
+// one waits for the one before (a third sum of eight channels apart cost 1.2
+// us of 12).
+template <int N> __device__ __forceinline__ void add_columns(float (&s)[N], int cols) {
+    const auto step = [&](auto f) {
+#pragma unroll
+        for (int j = 0; j < N; ++j) s[j] = f(s[j]);
+    };
+    if (cols <= 8) step([](float x) { return turned_sum<8>(x); });
+    if (cols <= 4) step([](float x) { return turned_sum<4>(x); });
+    if (cols <= 2) step([](float x) { return turned_sum<2>(x); });
+    if (cols <= 1) step([](float x) { return turned_sum<1>(x); });
+    if (cols <= 16) step([](float x) { return lane_step<16>(x); });
+    if (cols <= 32) step([](float x) { return lane_step<32>(x); });
+}
+// Those sums of N / V values of each of the V channels, left in `buf`: for
+// each value sum_rows(q) rows of `tile`.
 __device__ __forceinline__ int span_log2(const Cols& q) { return q.cols_log2 > 6 ? q.cols_log2 : 6; }
 __device__ __forceinline__ int sum_rows(const Cols& q) { return int(blockDim.x >> span_log2(q)); }
-template <int V>
-__device__ __forceinline__ void wave_channels(float (&s)[V], const Cols& q, int width, float* buf) {
+template <int V, int N>
+__device__ __forceinline__ void wave_channels(float (&s)[N], const Cols& q, int width, float* buf) {
     const int cols = 1 << q.cols_log2, col = int(threadIdx.x) & (cols - 1);
-    // the lanes of a row of 16 by turning it, which keeps the columns below the turn apart
-#pragma unroll
-    for (int j = 0; j < V; ++j) {
-        if (cols <= 8) s[j] = turned_sum<8>(s[j]);
-        if (cols <= 4) s[j] = turned_sum<4>(s[j]);
-        if (cols <= 2) s[j] = turned_sum<2>(s[j]);
-        if (cols <= 1) s[j] = turned_sum<1>(s[j]);
-        if (cols <= 16) s[j] = lane_step<16>(s[j]);
-        if (cols <= 32) s[j] = lane_step<32>(s[j]);
-    }
+    add_columns(s, cols);
     if (int(threadIdx.x & 63u) < cols && col * V < width) {
         float* to = buf + int(threadIdx.x >> span_log2(q)) * q.tile + col * V;
 #pragma unroll
-        for (int j = 0; j < V; ++j) to[j] = s[j];
+        for (int j = 0; j < N; ++j) to[(j / V) * sum_rows(q) * q.tile + j % V] = s[j];
     }
 }
 __device__ __forceinline__ float sum_of_channel(const float* buf, const Cols& q, int k) {

@@ -17,17 +17,15 @@ __global__ __launch_bounds__(1024) void k_gn_combine_fwd(const float4* __restric
     float sum = 0.f, num = 0.f;
 #pragma unroll 4
     for (int i = threadIdx.x; i < per; i += blockDim.x) {
-        sum = fmaf(p[i].z, p[i].x, sum);
-        num += p[i].z;
+        const float4 t = p[i];
+        sum = sum_with(t, sum);
+        num += t.z;
     }
     const float2 both = block_sum2(num, sum, part);
     const float mu = both.y / both.x;
     float sq = 0.f;
 #pragma unroll 4
-    for (int i = threadIdx.x; i < per; i += blockDim.x) {
-        const float d = p[i].x - mu;
-        sq += fmaf(p[i].z * d, d, p[i].y);
-    }
+    for (int i = threadIdx.x; i < per; i += blockDim.x) sq += squares_about(p[i], mu);
     sq = block_sum(sq, again);
     if (threadIdx.x == 0) {
         const float2 ms = stats_of(mu, sq / both.x, eps);

@@ -274,16 +274,16 @@ template <int DT, int V, int K>
 __global__ __launch_bounds__(256, 4) void k_gn_colparts_fwd(const typename Elt<DT>::T* __restrict__ x, Cols q, int images,
                                                          float4* __restrict__ parts) {
     using P = Pack<DT, V>;
-    extern __shared__ float lds[];              // two each: the waves' sums, the channels' means
+    extern __shared__ float lds[];              // the waves' sums, three, and the channels' means
     Place p;
     if (!place<V>(q, images, p)) return;
     const int all = sum_rows(q) * q.tile;
-    float* ch = lds + 2 * all;
+    float* ch = lds + 3 * all;
     const int64_t at = base_of(q, p);
     const typename Elt<DT>::T* xb = x + at;
     typename P::R d[K];
     each<DT, K>(q, p, [&](int i, uint32_t byte) { d[i] = get<typename P::R, false>(xb, byte); });
-    float s[V], mu[V];
+    float s[V], mu[V], both[2 * V];             // squares about the mean, and what it lacks
 #pragma unroll
     for (int j = 0; j < V; ++j) s[j] = 0.f;
     each<DT, K>(q, p, [&](int i, uint32_t) {
@@ -300,7 +300,7 @@ __global__ __launch_bounds__(256, 4) void k_gn_colparts_fwd(const typename Elt<D
 #pragma unroll
     for (int j = 0; j < V; ++j) {
         mu[j] = p.on ? ch[p.rel + j] : 0.f;
-        s[j] = 0.f;
+        both[j] = both[V + j] = 0.f;
     }
     each<DT, K>(q, p, [&](int i, uint32_t) {
         float f[V];
@@ -308,14 +308,15 @@ __global__ __launch_bounds__(256, 4) void k_gn_colparts_fwd(const typename Elt<D
 #pragma unroll
         for (int j = 0; j < V; ++j) {
             const float e = f[j] - mu[j];
-            s[j] = fmaf(e, e, s[j]);
+            both[j] = fmaf(e, e, both[j]);
+            both[V + j] += e;
         }
     });
-    wave_channels<V>(s, q, p.width, lds + all);
+    wave_channels<V>(both, q, p.width, lds + all);
     __syncthreads();
     for (int c = threadIdx.x; c < p.width; c += blockDim.x)
         parts[(int64_t(p.n) * q.c + p.c0 + c) * q.chunks + p.chunk] =
-            make_float4(ch[c], sum_of_channel(lds + all, q, c), num, 0.f);
+            make_float4(ch[c], sum_of_channel(lds + all, q, c), num, sum_of_channel(lds + 2 * all, q, c) * __builtin_amdgcn_rcpf(num));
 }
 
 // Calls f(group, lane) with a run of q.join_lanes lanes for each of the block's groups.
@@ -459,7 +460,7 @@ void fwd(const Plan& p, int n, const void* x, const Params& q, float eps, void* 
     T* yt = static_cast<T*>(y);
     const dim3 grid(static_cast<unsigned>(p.grid)), block(static_cast<unsigned>(p.threads));
     if (!p.held)
-        hipLaunchKernelGGL((k_gn_colparts_fwd<DT, V, piece_of(DT, V)>), grid, block, cols_lds(p.cols, p.threads, 2, 1), st, xt,
+        hipLaunchKernelGGL((k_gn_colparts_fwd<DT, V, piece_of(DT, V)>), grid, block, cols_lds(p.cols, p.threads, 3, 1), st, xt,
                            p.cols, n, parts);
     if (!p.held && !p.joined) combine_fwd(parts, int64_t(n) * p.cols.groups, p.cols.cg * p.pieces, eps, mean, rstd, st);
     with_act(q.act, [&](auto act) {

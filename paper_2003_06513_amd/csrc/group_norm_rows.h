@@ -218,7 +218,7 @@ template <int DT, int V, class F> void with_piece(int vpr, F go) {
     else go(IntC<n>{});
 }
 
-// The mean of the elements, their squares about it, and their number.
+// The mean of the elements, their squares about it, their number, and what the mean lacks.
 template <int DT, int V, bool MASK, int K>
 __global__ __launch_bounds__(256, 4) void k_gn_rowparts_fwd(const typename Elt<DT>::T* __restrict__ x, Rows s, int pieces,
                                                          unsigned count, float4* __restrict__ parts) {
@@ -228,30 +228,32 @@ __global__ __launch_bounds__(256, 4) void k_gn_rowparts_fwd(const typename Elt<D
     const PieceBase<V, MASK> b(s, int64_t(p.row) * s.hw, p.piece * K * 64);
     typename P::R d[K];
     each_of_piece<V, MASK, K>(b, [&](int i, const Window& w, bool) { d[i] = load<DT, V, MASK, false>(x, b, w); });
-    float sum = 0.f, num = 0.f;
+    const int most = K * 64 * V, have = (b.left < most ? b.left : most) - (MASK && b.first ? b.phase : 0);
+    const float num = have > 0 ? float(have) : 0.f;
+    float sum = 0.f;
     each_of_piece<V, MASK, K>(b, [&](int i, const Window& w, bool on) {
         float f[V], t = 0.f;
         P::open(d[i], f);
-        num += on ? float(w.hi - w.lo) : 0.f;
 #pragma unroll
         for (int j = 0; j < V; ++j) t += in<MASK>(w, j) ? f[j] : 0.f;
         sum += on ? t : 0.f;
     });
-    num = wave_sum(num);
     const float mu = num > 0.f ? wave_sum(sum) / num : 0.f;
-    float sq = 0.f;
+    float sq = 0.f, rest = 0.f;
     each_of_piece<V, MASK, K>(b, [&](int i, const Window& w, bool on) {
-        float f[V], t = 0.f;
+        float f[V], t = 0.f, u = 0.f;
         P::open(d[i], f);
 #pragma unroll
         for (int j = 0; j < V; ++j) {
             const float e = in<MASK>(w, j) ? f[j] - mu : 0.f;
             t = fmaf(e, e, t);
+            u += e;
         }
         sq += on ? t : 0.f;
+        rest += on ? u : 0.f;
     });
-    sq = wave_sum(sq);
-    if ((threadIdx.x & 63) == 0) parts[p.id] = make_float4(mu, sq, num, 0.f);
+    sq = wave_sum(sq), rest = wave_sum(rest);
+    if ((threadIdx.x & 63) == 0) parts[p.id] = make_float4(mu, sq, num, num > 0.f ? rest * __builtin_amdgcn_rcpf(num) : 0.f);
 }
 
 __device__ __forceinline__ Coeff coeff_of(const Piece& p, const Params& q, const float* mean, const float* rstd) {

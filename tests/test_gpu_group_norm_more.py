@@ -2,8 +2,9 @@
 import numpy as np
 import pytest
 
+from oracle import train
 from paper_2003_06513_amd import binding as B
-from gpu_cases import dev, note, torch_mod
+from gpu_cases import U32, dev, note, torch_mod
 from test_gpu_group_norm import (EPS, _data, _guards_hold, _need_gpu, _place, check_backward,        # noqa: F401
                                  check_forward)
 
@@ -126,3 +127,25 @@ def test_every_form(layout, dtype, shape, groups, shift):
         _guards_hold(tdx, bx, shift)
         check_backward(x, dy, groups, gamma, beta, hm, hr, act, tdx.cpu().numpy(), dgamma.cpu().numpy(),
                        dbeta.cpu().numpy(), what)
+
+
+# In pieces: joined by those who write them, or by a launch of its own; single elements (shift 1 of one tensor alone).
+@pytest.mark.parametrize("layout", ["nchw", "nhwc"])
+@pytest.mark.parametrize("shape,groups,shift", [((2, 32, 64, 64), 1, 0), ((1, 64, 300, 300), 1, 0), ((1, 4, 120, 150), 2, 0),
+                                                ((30, 64, 9, 9), 32, 1), ((3, 24, 50, 50), 2, 1)])
+def test_spread_far_from_zero(shape, groups, shift, layout):
+    """Levels of up to 10^4 spreads, and channels that differ: rstd is off by the square of the mean's error (in spreads)
+    and the roundings of sums of at most 64 values a lane, 64 a lane of the join and the trees: 160 u."""
+    torch = torch_mod()
+    for level in (0, 30, 100, 1000, 10000):
+        x, _, _, _ = _data(shape, np.float32, 39)
+        x = (x + np.float32(level)).astype(np.float32)
+        (tx, _), (ty, _) = _place(x, layout), _place(np.zeros_like(x), layout, shift)
+        mean, rstd = (torch.empty((shape[0], groups), device="cuda") for _ in range(2))
+        note("spread far from zero %s %s level %g" % (shape, layout, level))
+        B.group_norm_fwd(tx, groups, None, None, ty, mean=mean, rstd=rstd)
+        torch.cuda.synchronize()
+        rmean, rrstd = train.statistics(x, groups, 1e-5)
+        off = np.abs(mean.cpu().numpy() - rmean) * rrstd
+        err = np.abs(rstd.cpu().numpy() / rrstd - 1)
+        assert (err <= 160 * U32 + off ** 2).all(), (level, err.max(), off.max())
