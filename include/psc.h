@@ -291,7 +291,8 @@ psc_status psc_conv3x3_bwd_weight(const psc_layer *layer, const psc_packed *pack
  * c / groups neighbouring channels, over its M = c / groups * h * w values:
  *   mean = sum x / M,  rstd = 1 / sqrt(sum (x - mean)^2 / M + eps),
  *   xhat = (x - mean) rstd,  u = gamma[c] xhat + beta[c],  y = act(u)
- * with act(u) = u, max(u, 0) or u / (1 + exp(-u)).  Nothing that a call writes
+ * with act(u) = u, max(u, 0) or u / (1 + exp(-u)).  n and c are at most 65535, h
+ * and w 32768, a tensor holds fewer than 2^31 values.  Nothing that a call writes
  * (outputs, statistics, gradients, workspace) may overlap anything else of it. */
 typedef enum { PSC_NCHW = 0, PSC_NHWC = 1 } psc_layout;
 typedef enum { PSC_ACT_NONE = 0, PSC_ACT_RELU = 1, PSC_ACT_SILU = 2 } psc_act;

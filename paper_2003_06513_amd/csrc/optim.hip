@@ -9,6 +9,10 @@
 // The tensors' addresses travel in the kernel's arguments (a table of up to
 // kMaxEntries), so nothing is kept between calls and a captured launch holds
 // all it needs.
+//
+// The times in these comments compare two forms in one sitting.  From sitting to
+// sitting the largest differ by some percent (64 x 512 x 512 x 9 with 8 bits: 443
+// to 480 us).
 #include <cmath>
 #include <cstring>
 
