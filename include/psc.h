@@ -394,9 +394,9 @@ psc_status psc_grad_norm(const psc_param *h_params, int32_t count, float scale, 
  * parameter's update takes them before they become codes, in fp32 (m rounded
  * to it; sqrt(v) of the fp64 value, to fp32's precision).  sqrt|m| and v^(1/4)
  * are rounded to the nearest code, from the middle between two to the larger;
- * v > 0 keeps a code above 0.  A gradient that is
- * not finite, or whose (1 - beta2) g^2 passes fp32, spoils the moments of its
- * 256 elements (with 32 bits: its own). */
+ * v > 0 keeps a code above 0.  A gradient that is not finite, or whose
+ * (1 - beta2) g^2 passes fp32, spoils the moments of its 256 elements (with 32
+ * bits: its own). */
 #define PSC_ADAMW_STATE_BYTES 4352
 psc_status psc_adamw_step(const psc_param *h_params, int32_t count, const psc_adamw *opt,
                           const float *d_factor, void *d_state, void *stream);

@@ -256,11 +256,12 @@ __device__ __forceinline__ void param_block(const Tail& t) {
 
 // mean and rstd as they are kept: both NaN where a value of the group is not
 // finite, or a sum passed fp32 (then the variance is not finite, whatever the
-// mean is).
+// mean is).  That of joined pieces without a spread, all of it roundings of
+// their means, may round below zero, by more than a tiny eps.
 __device__ __forceinline__ float2 stats_of(float mu, float var, float eps) {
     const bool fine = __builtin_isfinite(var);
     const float nan = __builtin_nanf("");
-    return make_float2(fine ? mu : nan, fine ? 1.f / sqrtf(var + eps) : nan);
+    return make_float2(fine ? mu : nan, fine ? 1.f / sqrtf((var < 0.f ? 0.f : var) + eps) : nan);
 }
 
 // A piece in the sums of its group: mean x (rounded, and w what that lacks of

@@ -149,3 +149,23 @@ def test_spread_far_from_zero(shape, groups, shift, layout):
         off = np.abs(mean.cpu().numpy() - rmean) * rrstd
         err = np.abs(rstd.cpu().numpy() / rrstd - 1)
         assert (err <= 160 * U32 + off ** 2).all(), (level, err.max(), off.max())
+
+
+@pytest.mark.parametrize("layout", ["nchw", "nhwc"])
+@pytest.mark.parametrize("shape,groups,shift", [((3000, 3, 7, 11), 1, 1), ((300, 6, 37, 41), 2, 1), ((200, 12, 9, 5), 3, 0),
+                                                ((30, 32, 61, 67), 1, 0), ((20, 64, 300, 30), 1, 0)])
+def test_constant_groups_with_the_least_eps(shape, groups, shift, layout):
+    """No spread, and an eps far below the square of a rounding of the mean: a variance that rounds below zero would
+    make NaN of it.  The mean is the constant to within the roundings of the sums (and of the pieces' own means)."""
+    torch = torch_mod()
+    rng = np.random.default_rng(40)
+    value = (10.0 ** rng.uniform(-12, 7, shape[0]) * rng.choice([-1.0, 1.0], shape[0])).astype(np.float32)
+    value[:3] = 0, 1e-20, 0.1
+    x = np.broadcast_to(value[:, None, None, None], shape).copy()
+    (tx, _), (ty, _) = _place(x, layout), _place(np.zeros_like(x), layout, shift)
+    mean, rstd = (torch.empty((shape[0], groups), device="cuda") for _ in range(2))
+    note("constant groups %s %s" % (shape, layout))
+    B.group_norm_fwd(tx, groups, None, None, ty, eps=1.2e-38, mean=mean, rstd=rstd)
+    torch.cuda.synchronize()
+    assert (np.abs(mean.cpu().numpy() - value[:, None]) <= 160 * U32 * np.abs(value[:, None])).all()
+    assert bool(torch.isfinite(rstd).all()) and bool((rstd > 0).all()) and bool(torch.isfinite(ty).all())
