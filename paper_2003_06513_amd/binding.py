@@ -906,19 +906,20 @@ class AdamW:
         self.norm, self.factor = self._out[:1], self._out[1:]
         self._ws = torch.empty(GRAD_NORM_WS_BYTES, dtype=torch.uint8, device=device)
         self._at = self._state.get_device()
-        self._home = _stream(None, self._at)        # the stream whose pool all of this came from
+        self._streams = {_stream(None, self._at)}   # whose pool all of this came from, and those it is held for
 
     def _hold(self, stream):
         """Work on another stream than the one that the memory came from, be it
         the current one or named: it is not given out again before that is
         done.  (Work that is captured runs when and where it is replayed.)"""
-        if stream is None:
-            if _CURRENT(self._at) == self._home or _torch().cuda.is_current_stream_capturing():
-                return
+        handle = _CURRENT(self._at) if stream is None else stream.cuda_stream
+        if handle in self._streams or (stream is None and _torch().cuda.is_current_stream_capturing()):
+            return
         s = _torch_stream(stream)
         for t in (self.m, self.v, self.scale, self._state, self._out, self._ws):
             if t is not None:
                 t.record_stream(s)
+        self._streams.add(handle)
 
     def grad_norm(self, max_norm: float = float("inf"), scale: float = 1.0, stream=None):
         """The norm of the gradients and the factor that clips them, which

@@ -68,19 +68,27 @@ def test_optimiser_memory_is_held_for_the_stream_that_works_on_it(monkeypatch):
 
     opt = B.AdamW.__new__(B.AdamW)
     opt.m, opt.v, opt.scale, opt._state, opt._out, opt._ws = Buffer(), Buffer(), None, Buffer(), Buffer(), Buffer()
-    opt._at, opt._home = 0, 10
+    opt._at, opt._streams = 0, {10}
     now, capturing = [10], [False]
     B._torch()
     monkeypatch.setattr(B, "_CURRENT", lambda device: now[0])
-    monkeypatch.setattr(B, "_torch_stream", lambda stream: now[0] if stream is None else stream)
+    monkeypatch.setattr(B, "_torch_stream", lambda stream: now[0] if stream is None else stream.cuda_stream)
     monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: capturing[0])
+
+    class Stream:
+        def __init__(self, handle):
+            self.cuda_stream = handle
+
     opt._hold(None)
     assert held == []
-    now[0] = 11
+    now[0], capturing[0] = 11, True
+    opt._hold(None)
+    assert held == []
+    capturing[0] = False
     opt._hold(None)
     assert held == [11] * 5
-    capturing[0] = True
-    opt._hold(None)
+    for s in (None, Stream(10), Stream(11)):        # its own, and what it is held for already
+        opt._hold(s)
     assert held == [11] * 5
-    opt._hold(12)
+    opt._hold(Stream(12))
     assert held[5:] == [12] * 5
