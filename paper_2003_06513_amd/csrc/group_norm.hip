@@ -127,7 +127,7 @@ Plan plan_rows(const GroupNormArgs& a, bool backward, int vec) {
 int64_t cols_grid(Cols& s, int n, int elt) {
     s.near = 128 / (s.tile * elt);
     if (s.near < 1) s.near = 1;
-    // whole images, where every die gets as many of them (48 x 512 x 28 x 28 fp32 backward 67 -> 56 us)
+    // whole images, where every die gets as many of them, or many (48 x 512 x 28 x 28 fp32 backward 67 -> 56 us)
     const int64_t images = int64_t(n) * s.chunks;
     if (s.near > s.tiles || images >= 64 || (images >= 16 && images % 8 == 0)) s.near = s.tiles;
     // slabs alike: of 12 tiles 6 and 6, not 8 and 4 (20 x 96 x 40 x 40 fp16 14.5 -> 12 us)
@@ -141,7 +141,8 @@ int64_t cols_grid(Cols& s, int n, int elt) {
 // are faster once there are more blocks than CUs (forward, 20 x 256 x 56 x 56
 // fp32: 42 us in pieces, 57 held; 40 x 128 x 40 x 40 fp16: 14 in 160 blocks, 23
 // in 640), in the backward in tiles of 16 bytes also before (64 x 64 x 56 x
-// 56 fp16: 33 us in pieces, 41 held).
+// 56 fp16: 33 us in pieces, 41 held).  The limits lie between measured sides
+// such as these; no model of the caches stands behind them.
 bool narrow_loses(int64_t units, int threads, int64_t k, int bytes, bool wider, bool backward, int piece) {
     const bool many = units > 256;
     if (!backward) return many && (wider || 2 * k >= piece);
